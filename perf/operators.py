@@ -295,8 +295,8 @@ def _run_own(s):
         return sdnn.sdnn_unpack8(packed, x=s["out"])
     net = s["net"]
     net.sdnn_checkpoint_load(s["kept"], case["batch"])
-    net.sdnn_backward(s["dloss"])
-    return [net.sdnn_weight_grad(l + 1) for l in range(case["layers"])], net.sdnn_input_grad(case["batch"], dx0=s["out"])
+    dx0 = net.sdnn_backward_input(s["dloss"], s["out"])
+    return [net.sdnn_weight_grad(l + 1) for l in range(case["layers"])], dx0
 
 
 def run(state):
