@@ -19,7 +19,7 @@
  * f'(z) is 1 for 0 < z < act_cap and 0 elsewhere (sigmoid: x(1-x)); it is
  * evaluated from the stored output x = f(z).  Back-propagation uses the weights of the forward
  * pass (Algorithm 1 forms delta^{k-1} before it updates W^k); every update is
- * applied by sdnn_sgd_step.  Delta_0 is not formed.
+ * applied by sdnn_sgd_step.  Delta_0 is not formed (sdnn_backward_input forms W_1^T Delta_1).
  *
  * Arithmetic: fp32 storage, every sum accumulated in fp64 and rounded once
  * when stored.  No sum and no result goes through an atomic operation: results
@@ -221,9 +221,69 @@ int sdnn_forward_skip_dead(sdnn_net *net, const float *d_X0, int32_t B, float *d
  * forward call that must directly precede it.  Training mode only. */
 int sdnn_backward(sdnn_net *net, const float *d_dLoss, void *stream);
 
+/* sdnn_backward that also forms the gradient of the net's input, for what comes below the net (a layer norm, another net):
+ * d_dX0 [n_in(1)][B] = dJ/dX_0 = W_1^T Delta_1, without a derivative factor (X_0 is no activation of this net's).  Everything else
+ * is as after sdnn_backward, to the bit.  Where the sweep of the first layer gathers Delta_1 for the gradient anyway, d_dX0
+ * is formed in it; else it is one more product.  d_dX0 must not overlap d_dLoss. */
+int sdnn_backward_input(sdnn_net *net, const float *d_dLoss, float *d_dX0, void *stream);
+
 /* Eqs. 4-5 on every layer, confined to the stored pattern.  Needs a preceding
  * sdnn_backward and consumes it (a second step is SDNN_ESTATE). */
 int sdnn_sgd_step(sdnn_net *net, float lr, void *stream);
+
+/* ---- activations in 8 bits -------------------------------------------------
+ * A training net keeps the X_0..X_L of ONE batch, in fp32.  Who runs further batches forward before the first one's backward pass
+ * (micro-batches in a pipeline, a net that is used at two places) puts them away, in a quarter of the bytes:
+ *
+ *   sdnn_forward(net, batch 1); sdnn_checkpoint_save(net, c1);  sdnn_forward(net, batch 2); sdnn_checkpoint_save(net, c2);  ...
+ *   sdnn_checkpoint_load(net, c1, B1); sdnn_backward(net, dLoss 1); sdnn_weight_grad or sdnn_sgd_step;  ...
+ *
+ * A packed block of X [n][B]: a byte for every value, in the order of the block, filled up to whole groups of 128 bytes; then a scale
+ * of 16 bits for every group (a bf16: the upper half of an fp32); filled up with anything to a multiple of 256 bytes.  The scale t is
+ * the smallest one for which the group's largest value fits; values go to the nearest multiple of t, halves away from zero.
+ *   cap = 0  values of both signs, -127 t .. 127 t as signed bytes; -128: infinite or NaN, comes back as NaN
+ *   cap > 0  activations 0 <= x <= cap (smaller ones count as 0; cap may be +INFINITY): byte 0: 0; 255: cap; 254: NaN; 1..253: that many t,
+ *            for every 0 < x < cap: none becomes 0 or cap, so that f' of the clamped ReLU is exact
+ * A value moves by at most t / 2 (with a cap, values below t / 2 by less than t), t <= 1.008 max / 127 or 1.008 max / 253 of its group. */
+
+/* Bytes of a packed block (n >= 0, B >= 1, n B < 2^40; 0 for n = 0). */
+int sdnn_pack8_bytes(int32_t n, int32_t B, size_t *bytes);
+/* d_packed: packed_bytes >= those bytes (SDNN_ENOMEM otherwise), aligned to 16. */
+int sdnn_pack8(const float *d_X, int32_t n, int32_t B, float cap, void *d_packed, size_t packed_bytes, void *stream);
+int sdnn_unpack8(const void *d_packed, size_t packed_bytes, int32_t n, int32_t B, float cap, float *d_X, void *stream);
+
+/* A checkpoint is the packed blocks of X_0 (cap = 0), X_1, .., X_L (cap = act_cap; 1 for the sigmoid) one after the other, each of
+ * sdnn_pack8_bytes(its neurons, B): X_l's block can be handed to the functions of single blocks.  Training nets only. */
+int sdnn_checkpoint_bytes(const sdnn_net *net, int32_t B, size_t *bytes);
+/* Directly after sdnn_forward or sdnn_checkpoint_load (SDNN_ESTATE otherwise), of their B.  d_ckpt: ckpt_bytes >= sdnn_checkpoint_bytes
+ * (SDNN_ENOMEM otherwise), aligned to 16.  Does not change the net: sdnn_backward may follow. */
+int sdnn_checkpoint_save(sdnn_net *net, void *d_ckpt, size_t ckpt_bytes, void *stream);
+/* X_0..X_L become what the checkpoint of B samples holds, as if sdnn_forward had left them: sdnn_backward and what
+ * builds on it may follow.  The weights are those of the time of the backward pass. */
+int sdnn_checkpoint_load(sdnn_net *net, const void *d_ckpt, size_t ckpt_bytes, int32_t B, void *stream);
+
+/* ---- layer norm -------------------------------------------------------------
+ * Over the neurons of each sample of a block [n][B] (before a net, between two nets):
+ *   m_s = 1/n sum_i X(i,s),  v_s = 1/n sum_i (X(i,s) - m_s)^2,  r_s = 1/sqrt(v_s + eps)
+ *   Y(i,s) = gamma(i) h(i,s) + beta(i),  h(i,s) = (X(i,s) - m_s) r_s
+ * and back, with the gradients of gamma and beta, from dY:
+ *   dX(i,s) = r_s (gamma(i) dY(i,s) - 1/n sum_k gamma(k) dY(k,s) - h(i,s) 1/n sum_k gamma(k) dY(k,s) h(k,s))
+ *   dgamma(i) = sum_s dY(i,s) h(i,s),  dbeta(i) = sum_s dY(i,s)
+ * d_gamma, d_beta [n] or NULL (ones, zeros).  d_stats: double [2][B], m and then r, written by the forward pass (NULL: not wanted) and
+ * read by the backward pass.  eps > 0.  A sample that holds an infinity or NaN becomes NaN, and no other does.
+ * 1 <= n, B <= 2^30, n B < 2^40.  d_work: sdnn_layernorm_workspace_bytes (SDNN_ENOMEM if work_bytes is less), aligned to 16; its contents
+ * do not matter, and calls that share it must be ordered (two graphs that are replayed at a time need one each). */
+int sdnn_layernorm_workspace_bytes(int32_t n, int32_t B, size_t *bytes);
+/* d_Y may be d_X (and must not overlap it otherwise). */
+int sdnn_layernorm(const float *d_X, const float *d_gamma, const float *d_beta, int32_t n, int32_t B, double eps, float *d_Y,
+                   double *d_stats, void *d_work, size_t work_bytes, void *stream);
+/* d_dX [n][B], d_dgamma [n], d_dbeta [n]: NULL where not wanted, one at least given.  d_dX may be d_dY (or, where X is not in 8 bits, d_X). */
+int sdnn_layernorm_backward(const float *d_dY, const float *d_X, const double *d_stats, const float *d_gamma, int32_t n, int32_t B,
+                            float *d_dX, float *d_dgamma, float *d_dbeta, void *d_work, size_t work_bytes, void *stream);
+/* The same with X as a packed block (of cap as above), which is read as it is: h is formed from the values that the bytes stand for. */
+int sdnn_layernorm_backward_packed(const float *d_dY, const void *d_packed, size_t packed_bytes, float cap, const double *d_stats,
+                                   const float *d_gamma, int32_t n, int32_t B, float *d_dX, float *d_dgamma, float *d_dbeta,
+                                   void *d_work, size_t work_bytes, void *stream);
 
 /* ---- inspection (parity tests, checkpoints) ------------------------------
  * All copy into caller-provided DEVICE buffers on `stream`. */

@@ -7,7 +7,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsdnn.so")
-SOURCES = ["sdnn.hip", "sdnn_setup.cpp"]
+SOURCES = ["sdnn.hip", "sdnn_norm.hip", "sdnn_pack.hip", "sdnn_setup.cpp"]
 
 # packed-fp32 instruction selection is switched off for all device code; k_fwd_pan's inline assembly clobbers m0 and registers
 # that it keeps from the compiler, on purpose

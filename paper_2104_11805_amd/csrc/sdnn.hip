@@ -116,8 +116,10 @@ __device__ __forceinline__ void gatherv(__amdgpu_buffer_rsrc_t r, unsigned lane_
 // Activations (the paper's Eq. 3 leaves f open; Section 6.1 trains with the sigmoid).
 //   ACT_RELU_CAP: f(z) = min(max(z, 0), cap), f' = [0 < x < cap] from the stored output x
 //   ACT_SIGMOID:  f(z) = 1 / (1 + exp(-z)),   f' = x (1 - x)     from the stored output x
+//   ACT_NONE:     f' = 1, for what lies below the net (dJ/dX_0)
 #define ACT_RELU_CAP 0
 #define ACT_SIGMOID 1
+#define ACT_NONE 2
 __device__ __forceinline__ float act_apply(int act, double z, float capf)
 {
     if (act == ACT_SIGMOID) return (float)(1.0 / (1.0 + exp(-z)));
@@ -133,7 +135,7 @@ __device__ __forceinline__ float act_backprop(int act, double value, float x, fl
         const double xd = (double)x;
         return (float)(value * (xd * (1.0 - xd)));
     }
-    return (x > 0.0f && x < capf) ? (float)value : 0.0f;
+    return (x > 0.0f && x < capf) || act == ACT_NONE ? (float)value : 0.0f;
 }
 
 // Orders the LDS (or in-place global) accesses of the lanes of one wavefront: what the lanes wrote before
@@ -212,6 +214,7 @@ struct GradArgs : SpmmArgs {
     float *g_part[2];  // gradient of the stored entries over the samples of the first / second tile, in the order of the
                        // transposed index [nnz]
     int32_t store_out; // 0 = only the gradient is wanted (first layer: there is no Delta_0)
+    int32_t ld_dst;    // floats per row of `out` (ld_out: of X_{l-1})
 };
 static_assert(sizeof(SpmmArgs) == 128, "see above");
 
@@ -645,6 +648,24 @@ __device__ __forceinline__ float add_neighbour16(float g)
     return (float)((double)__uint_as_float(t[0]) + (double)__uint_as_float(t[1]));
 }
 
+// Four samples of a row of Delta_{l-1}, or of dJ/dX_0 in the caller's rows of B floats; zeros after the batch's last sample.
+__device__ __forceinline__ void store_group(const GradArgs &a, int row, int s, float (&o)[4])
+{
+    float *dst = a.out + (size_t)row * a.ld_dst + s;
+    if (((a.ld_dst & 3) | ((int)(size_t)a.out & 15)) == 0) {
+        if (s + 4 > a.B) { // the batch's last group
+#pragma unroll
+            for (int v = 1; v < 4; ++v)
+                if (s + v >= a.B) o[v] = 0.0f;
+        }
+        stv<4>(dst, o);
+    } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (s + v < a.B) dst[v] = o[v];
+    }
+}
+
 // The backward sweep that also forms the gradient of the stored entries, in the manner of k_rows.  The lanes of row i of
 // W_l^T hold X_{l-1}(i, :), four samples each, gather Delta_l(j, :) for every entry (j, i) and sum its products with
 // X_{l-1}(i, :) over the samples: four in the lane, the rest over the row's lanes, four entries at a time while the
@@ -728,12 +749,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_rows(const GradArgs a)
     float o[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) o[v] = act_backprop(a.act, acc[v], xp[v], a.cap);
-    if (s + 4 > a.B) { // the batch's last group
-#pragma unroll
-        for (int v = 1; v < 4; ++v)
-            if (s + v >= a.B) o[v] = 0.0f;
-    }
-    stv<4>(a.out + (size_t)row * a.ld_out + s, o);
+    store_group(a, row, s, o);
 }
 
 // The same sweep for long rows and more than 128 samples: a wavefront per row.  k_bwd_rows<64> keeps the vector units issuing in
@@ -853,12 +869,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_long(const GradArgs a)
     float o[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) o[v] = act_backprop(a.act, acc[v], xp[v], a.cap);
-    if (s + 4 > a.B) { // the batch's last group
-#pragma unroll
-        for (int v = 1; v < 4; ++v)
-            if (s + v >= a.B) o[v] = 0.0f;
-    }
-    stv<4>(a.out + (size_t)row * a.ld_out + s, o);
+    store_group(a, row, s, o);
 }
 
 // ---------------------------------------------------------------------------
@@ -1552,6 +1563,27 @@ __global__ void __launch_bounds__(256) k_train_turn(const LayerDev *__restrict__
     }
 }
 
+// And from X_l back to [step][max_batch][position], where the backward pass reads it, after X_l came from a checkpoint.
+__global__ void __launch_bounds__(256) k_train_unturn(const LayerDev *__restrict__ layers, int step0, const LmLayer *__restrict__ tab,
+                                                      const int32_t *__restrict__ rows, float *__restrict__ to, int max_batch, int ld, int B)
+{
+    __shared__ float tile[64][65];
+    const int k = step0 + (int)blockIdx.z, tid = threadIdx.x, p0 = 64 * blockIdx.x, s0 = 64 * blockIdx.y;
+    const LmLayer t = tab[k];
+    if (p0 >= t.n_pos) return;
+    const float *in = layers[k].X;
+    float *out = to + (size_t)t.pos * max_batch;
+    for (int i = tid; i < 4096; i += 256) {
+        const int s = i & 63, p = i >> 6, row = rows[t.pos + p0 + p];
+        tile[s][p] = row >= 0 && s0 + s < B ? in[(size_t)row * ld + s0 + s] : 0.0f;
+    }
+    __syncthreads();
+    for (int i = tid; i < 4096; i += 256) {
+        const int p = i & 63, s = i >> 6;
+        if (s0 + s < B) out[(size_t)(s0 + s) * t.n_pos + p0 + p] = tile[s][p];
+    }
+}
+
 // Writes the weights of the steps' copies from the CSR values (COLS: and the positions of the operand), and the biases by position:
 // steps step0 .. step0 + n_steps - 1, eight steps to a row of the grid, each on an XCD of its own (MODE 1 reads a layer's values in
 // any order: by all XCDs 77 us for 120 layers of 1024 neurons).  grid = (8 max_nb wavefronts, eights of steps).  pos: the positions of every step's rows, step after step; first[k]: where
@@ -2148,8 +2180,8 @@ __device__ __forceinline__ void spmm_row_grad(RowMeta m, const GradArgs &a, int 
             wave_lds_sync(); // the next group's rows are parked over the ones just read
         }
     }
-    if (a.store_out && lane < (fills_up(B, a.ld_out) ? (B + 3) & ~3 : B))
-        a.out[(size_t)m.row * ld + lane] = live ? act_backprop(a.act, acc, xp, a.cap) : 0.0f;
+    if (a.store_out && lane < (fills_up(B, a.ld_dst) ? (B + 3) & ~3 : B))
+        a.out[(size_t)m.row * a.ld_dst + lane] = live ? act_backprop(a.act, acc, xp, a.cap) : 0.0f;
 }
 template <int U>
 __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_grad(const GradArgs a)
@@ -3195,6 +3227,8 @@ struct Plan {
 // in every X_l and Delta_l (the kernels store zeros for them: what a zero input turns into on its way may be infinite), so
 // that they add exact zeros to every gradient.
 static int padded_batch(int B) { return B == 1 ? 1 : (B + 3) & ~3; }
+// The same where rows of ld floats may have no room for them (row_pitch).
+static int padded_rows(int B, int ld) { return ld < padded_batch(B) ? B : padded_batch(B); }
 // Floats per row of the library's own activation and delta arrays: 16-byte pieces stay aligned, a row touches as few
 // 128-byte lines as it can.
 static int row_stride(int B)
@@ -4518,8 +4552,9 @@ static const void *rows_fn(int G, int act)
 template <int MODE>
 static int launch_spmm(sdnn_net *net, const LayerDev &d, const float *in, int ld_in, float *out, int ld_out,
                        const float *aux, int B, hipStream_t stream, const int32_t *n_live = nullptr, int32_t *flags = nullptr,
-                       int sub_begin = 0, int sub_end = 0)
+                       int sub_begin = 0, int sub_end = 0, int act = -1)
 {
+    if (act < 0) act = net->cfg.activation;
     if (sub_end == 0) sub_end = B;
     SpmmArgs a;
     a.n_live = n_live;
@@ -4532,7 +4567,7 @@ static int launch_spmm(sdnn_net *net, const LayerDev &d, const float *in, int ld
         a.n_rows = d.n_in;
     }
     a.vals = d.vals; a.in = in; a.out = out; a.aux = aux; a.B = B; a.ld_in = ld_in; a.ld_out = ld_out;
-    a.cap = net->cfg.act_cap; a.act = net->cfg.activation;
+    a.cap = net->cfg.act_cap; a.act = act;
     if (a.n_rows == 0) return SDNN_OK;
     const int n_cols = MODE == 0 ? d.n_in : d.n_out;
     a.n_cols = n_cols;
@@ -4930,7 +4965,7 @@ static int forward_impl(sdnn_net *net, const float *d_X0, int32_t B, float *d_XL
     }
     const float *in = d_X0;
     int ld_in = B;
-    const int Bp = ld < padded_batch(B) ? B : padded_batch(B);
+    const int Bp = padded_rows(B, ld);
     if (training) {
         const int rc = launch_copy_rows(net, d_X0, B, net->d_x0, ld, net->layers[0].n_in, B, Bp, stream);
         if (rc) return rc;
@@ -5179,19 +5214,27 @@ static bool bwd_long(const LayerDev &d, uint32_t in_bytes, int B)
     return mb <= (B > 224 ? 16.0 : 26.0) && (double)d.nnz >= std::max(64.0, 20.0 * mb - 150.0) * d.n_in;
 }
 
-// Fused back-propagation + entry gradient of one layer.  store_out = 0 for the first layer (gradient only: there is no
-// Delta_0, out may be NULL).
-static int launch_bwd_grad(sdnn_net *net, const LayerDev &d, float *out, hipStream_t stream, int store_out)
+// dJ/dX_0 = W_1^T Delta_1 by itself.  (The kernels read an operand for f' from where they store, and do without it.)
+static int launch_input_grad(sdnn_net *net, float *out, hipStream_t stream)
 {
+    const LayerDev &d = net->layers[0];
+    return launch_spmm<1>(net, d, d.D, net->ld, out, net->B, out, net->B, stream, nullptr, nullptr, 0, 0, ACT_NONE);
+}
+
+// Fused back-propagation + entry gradient of one layer.  out NULL, for the first layer: gradient only, there is no Delta_0;
+// else for the first layer the caller's dJ/dX_0.
+static int launch_bwd_grad(sdnn_net *net, const LayerDev &d, float *out, hipStream_t stream)
+{
+    const bool first = &d == net->layers.data();
     const int B = net->Bp;
     GradArgs a;
     a.row_ptr = d.t_row_ptr; a.idx = d.t_row_idx; a.perm = nullptr; a.sched = d.t_sched; a.n_rows = d.n_in;
     a.vals = d.vals_t; a.in = d.D; a.out = out; a.aux = d.X_prev; a.B = net->B; a.ld_in = a.ld_out = net->ld; a.cap = net->cfg.act_cap;
-    a.act = net->cfg.activation; a.n_live = nullptr; a.flags = nullptr;
-    a.g_part[0] = d.G[0]; a.g_part[1] = d.G[1]; a.store_out = store_out;
+    a.act = first ? ACT_NONE : net->cfg.activation; a.n_live = nullptr; a.flags = nullptr;
+    a.g_part[0] = d.G[0]; a.g_part[1] = d.G[1]; a.store_out = out ? 1 : 0; a.ld_dst = first ? net->B : net->ld;
     if (a.n_rows == 0 || d.nnz == 0) {
-        if (d.nnz == 0 && store_out && a.n_rows > 0) // no entries: Delta_{l-1} = 0, nothing to differentiate
-            return launch_spmm<1>(net, d, d.D, net->ld, out, net->ld, d.X_prev, net->B, stream);
+        if (d.nnz == 0 && out && a.n_rows > 0) // no entries: Delta_{l-1} = 0, nothing to differentiate
+            return first ? launch_input_grad(net, out, stream) : launch_spmm<1>(net, d, d.D, net->ld, out, net->ld, d.X_prev, net->B, stream);
         return SDNN_OK;
     }
     a.n_cols = d.n_out;
@@ -5241,7 +5284,7 @@ static int grad_fusable(const sdnn_net *net, int B)
     return net->two_windows && 4 * (int64_t)net->max_n * B > 6500000 ? 2 : 1;
 }
 
-extern "C" int sdnn_backward(sdnn_net *net, const float *d_dLoss, void *stream_)
+static int backward_impl(sdnn_net *net, const float *d_dLoss, float *d_dX0, void *stream_)
 {
     if (!net) return fail(nullptr, SDNN_EINVAL, "net is NULL");
     if (!net->cfg.training) return fail(net, SDNN_ESTATE, "net was not created for training");
@@ -5253,7 +5296,7 @@ extern "C" int sdnn_backward(sdnn_net *net, const float *d_dLoss, void *stream_)
     const LayerDev &last = net->layers[L - 1];
     net->two_windows = two_windows(net);
     const int gp = grad_fusable(net, B);
-    for (int l = gp ? 0 : 1; l < L; ++l) { // the operands of the products below: refused before anything is launched
+    for (int l = gp || d_dX0 ? 0 : 1; l < L; ++l) { // the operands of the products below: refused before anything is launched
         const LayerDev &d = net->layers[l];
         const size_t bytes = 4 * (size_t)d.n_out * (size_t)net->ld;
         if (d.n_in > 0 && (l > 0 || d.nnz > 0) && bytes >= ((size_t)1 << 32))
@@ -5285,12 +5328,104 @@ extern "C" int sdnn_backward(sdnn_net *net, const float *d_dLoss, void *stream_)
     for (int l = L - 1; l >= (gp ? 0 : 1) && !single; --l) {
         const LayerDev &d = net->layers[l];
         // Delta_{l} (0-based l-1) = (W^T Delta_{l+1}) masked by X_{l}
-        float *dprev = l >= 1 ? net->layers[l - 1].D : nullptr;
-        const int rc = gp ? launch_bwd_grad(net, d, dprev, stream, l >= 1)
+        float *dprev = l >= 1 ? net->layers[l - 1].D : d_dX0;
+        const int rc = gp ? launch_bwd_grad(net, d, dprev, stream)
                           : launch_spmm<1>(net, d, d.D, net->ld, dprev, net->ld, d.X_prev, net->B, stream);
         if (rc) return rc;
     }
+    if (d_dX0 && !gp) {
+        const int rc = launch_input_grad(net, d_dX0, stream);
+        if (rc) return rc;
+    }
     net->state = ST_BACKWARD;
+    return SDNN_OK;
+}
+
+extern "C" int sdnn_backward(sdnn_net *net, const float *d_dLoss, void *stream_) { return backward_impl(net, d_dLoss, nullptr, stream_); }
+
+extern "C" int sdnn_backward_input(sdnn_net *net, const float *d_dLoss, float *d_dX0, void *stream_)
+{
+    if (net && !d_dX0) return fail(net, SDNN_EINVAL, "d_dX0 is NULL");
+    return backward_impl(net, d_dLoss, d_dX0, stream_);
+}
+
+// ---------------------------------------------------------------------------
+// activations in 8 bits (the kernels: sdnn_pack.hip)
+// ---------------------------------------------------------------------------
+extern "C" int sdnn_checkpoint_bytes(const sdnn_net *net, int32_t B, size_t *bytes)
+{
+    if (!net || !bytes) return fail(nullptr, SDNN_EINVAL, "net or bytes is NULL");
+    if (!net->cfg.training) return fail(nullptr, SDNN_ESTATE, "net was not created for training");
+    if (B < 1 || B > net->cfg.max_batch) return fail(nullptr, SDNN_EINVAL, "B = %d outside 1..max_batch = %d", B, net->cfg.max_batch);
+    size_t total = 0;
+    for (int l = 0; l <= net->n_layers; ++l) {
+        size_t b = 0;
+        const int rc = sdnn_pack8_bytes(l == 0 ? net->layers[0].n_in : net->layers[l - 1].n_out, B, &b);
+        if (rc) return rc;
+        total += b;
+    }
+    *bytes = total;
+    return SDNN_OK;
+}
+
+// X_0 .. X_L of net->B samples into the checkpoint, or (restore) out of it.
+static int checkpoint(sdnn_net *net, void *d_ckpt, int restore, void *stream_)
+{
+    if (net->max_n == 0) return SDNN_OK;
+    const float cap = net->cfg.activation == ACT_SIGMOID ? 1.0f : net->cfg.act_cap;
+    HIP_TRY(net, (hipError_t)sdnn_launch_checkpoint(net->d_layers, net->d_x0, net->n_layers, net->max_n, net->B, net->Bp, net->ld, cap, d_ckpt, restore, stream_));
+    return SDNN_OK;
+}
+
+static int check_checkpoint(sdnn_net *net, const void *d_ckpt, size_t ckpt_bytes, int32_t B)
+{
+    size_t need = 0;
+    const int rc = sdnn_checkpoint_bytes(net, B, &need);
+    if (rc) {
+        snprintf(net->err, sizeof net->err, "%s", sdnn_global_error());
+        return rc;
+    }
+    if (need > 0 && !d_ckpt) return fail(net, SDNN_EINVAL, "d_ckpt is NULL");
+    if (!aligned(d_ckpt, 16)) return fail(net, SDNN_EINVAL, "d_ckpt must be 16-byte aligned");
+    if (ckpt_bytes < need) return fail(net, SDNN_ENOMEM, "checkpoint of %zu bytes, %zu needed", ckpt_bytes, need);
+    return SDNN_OK;
+}
+
+extern "C" int sdnn_checkpoint_save(sdnn_net *net, void *d_ckpt, size_t ckpt_bytes, void *stream_)
+{
+    if (!net) return fail(nullptr, SDNN_EINVAL, "net is NULL");
+    if (!net->cfg.training) return fail(net, SDNN_ESTATE, "net was not created for training");
+    if (net->state != ST_FORWARD) return fail(net, SDNN_ESTATE, "sdnn_checkpoint_save needs a directly preceding sdnn_forward");
+    const int rc = check_checkpoint(net, d_ckpt, ckpt_bytes, net->B);
+    return rc ? rc : checkpoint(net, d_ckpt, 0, stream_);
+}
+
+extern "C" int sdnn_checkpoint_load(sdnn_net *net, const void *d_ckpt, size_t ckpt_bytes, int32_t B, void *stream_)
+{
+    if (!net) return fail(nullptr, SDNN_EINVAL, "net is NULL");
+    if (!net->cfg.training) return fail(net, SDNN_ESTATE, "net was not created for training");
+    int rc = check_checkpoint(net, d_ckpt, ckpt_bytes, B);
+    if (rc) return rc;
+    const int ld = row_pitch(net->max_n, B);
+    for (const LayerDev &d : net->layers) // what sdnn_forward refuses
+        if (4 * (size_t)d.n_in * (size_t)ld >= ((size_t)1 << 32))
+            return fail(net, SDNN_EINVAL, "activation block of %zu bytes exceeds 4 GiB: use a smaller B", 4 * (size_t)d.n_in * (size_t)ld);
+    net->state = ST_IDLE;
+    net->B = B;
+    net->ld = ld;
+    net->Bp = padded_rows(B, ld);
+    rc = checkpoint(net, const_cast<void *>(d_ckpt), 1, stream_);
+    if (rc) return rc;
+    if (train_lds(net, B)) { // the backward pass in one launch reads X_l by position
+        const sdnn_net::Train &t = net->train[0];
+        const int n_steps = (int)t.tab.size();
+        for (int k0 = 0; k0 < n_steps; k0 += 65535) {
+            hipLaunchKernelGGL(k_train_unturn, dim3((unsigned)(LDS_WAVES * t.max_nb), (unsigned)((B + 63) / 64), (unsigned)std::min(65535, n_steps - k0)),
+                               dim3(256), 0, (hipStream_t)stream_, net->d_layers, k0, t.d_tab, t.row, t.out, net->cfg.max_batch, ld, B);
+            HIP_TRY(net, hipGetLastError());
+        }
+    }
+    net->state = ST_FORWARD;
     return SDNN_OK;
 }
 

@@ -72,3 +72,7 @@ struct PanLayout {
     double depth = 0;
 };
 void sdnn_pan_layout(const sdnn_layer &y, const PanLayer &g, PanLayout &out);
+
+// sdnn_pack.hip: X_0 .. X_L of a training net to (restore = 0) or from a checkpoint; returns a hipError_t.  max_n: neurons of the widest block
+int sdnn_launch_checkpoint(const LayerDev *d_layers, float *d_x0, int32_t n_layers, int64_t max_n, int32_t B, int32_t Bp, int32_t ld, float cap,
+                           void *d_ckpt, int restore, void *stream);

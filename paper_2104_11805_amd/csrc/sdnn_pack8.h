@@ -1,0 +1,71 @@
+// Blocks of activations in 8 bits, as the kernels read and write them (sdnn_pack.hip writes and restores them, the backward pass of
+// the layer norm reads them as they are).
+//
+// The values of a block [n][B], in its order, in groups of 128; a group has one scale t, a float of 8 significant bits (a bf16),
+// the smallest with  most t >= the group's largest value.  A value is stored as the nearest multiple of t, halves away from zero:
+//   cap == 0  both signs; most = 127: code c stands for c t, -128 for what is not finite
+//   cap > 0   0 <= x <= cap; most = 253: code 0 for 0, 255 for cap, 254 for NaN, and 1 .. 253 for 0 < x < cap (no such value becomes
+//             0, none becomes cap: the derivative of the clamped ReLU is exact)
+// c t is exact in fp32 (8 bits times 8 bits).  A value is off by at most t / 2 <= 0.4 % (cap: 0.2 %) of its group's largest, one
+// below t / 2 with a cap by less than t.
+#pragma once
+#include <cfloat>
+#include <cstdint>
+#include <hip/hip_runtime.h>
+
+#include "sdnn_internal.h"
+
+#define PACK_GROUP 128
+
+static inline int64_t pack8_groups(int64_t count) { return (count + PACK_GROUP - 1) / PACK_GROUP; }
+static inline int64_t pack8_bytes(int64_t count) { return ((PACK_GROUP + 2) * pack8_groups(count) + 255) & ~(int64_t)255; }
+
+// The scale of a group whose largest value is `largest`, as the 16 bits that are stored.
+__device__ __forceinline__ unsigned pack8_scale(float largest, float most)
+{
+    unsigned t = __float_as_uint(largest / most) >> 16; // that, or one or two more: division and cutting off lose
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+        if ((double)most * (double)__uint_as_float(t << 16) < (double)largest) ++t;
+    return t;
+}
+// What values are multiplied by before they are rounded: 1 / t, and 2^-40 of it more.  The nearest fp32 value to a half of t is 2^-24
+// of it away, so that halves, and nothing else, are lifted over the border that the rounding of this product could move.
+__device__ __forceinline__ double pack8_inverse(unsigned t)
+{
+    return t ? (1.0 + 0x1p-40) / (double)__uint_as_float(t << 16) : 0.0;
+}
+__device__ __forceinline__ bool pack8_live(float x, float cap)
+{
+    return cap > 0.0f ? x > 0.0f && x < cap : fabsf(x) <= FLT_MAX;
+}
+__device__ __forceinline__ unsigned pack8_code(float x, float cap, double inverse)
+{
+    const bool live = pack8_live(x, cap);
+    const int c = (int)fma(live ? (double)fabsf(x) : 0.0, inverse, 0.5);
+    if (cap > 0.0f) return live ? (unsigned)max(c, 1) : x >= cap ? 255u : x != x ? 254u : 0u;
+    return live ? (unsigned)(x < 0.0f ? -c : c) & 255u : 128u;
+}
+// below: the largest float below cap
+__device__ __forceinline__ float pack8_value(unsigned code, float scale, float cap, float below)
+{
+    if (cap > 0.0f) {
+        const float v = fminf((float)code * scale, below);
+        return code == 255u ? cap : code == 254u ? __builtin_nanf("") : v;
+    }
+    return code == 128u ? __builtin_nanf("") : (float)(int)(signed char)code * scale;
+}
+
+// ---- host side, shared by the operators on single blocks ----------------------------------------------------------------
+template <class... A> static inline int sdnn_fail(int code, const char *fmt, A... a)
+{
+    sdnn_set_global_error(fmt, a...);
+    return code;
+}
+static inline int sdnn_launched()
+{
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? SDNN_OK : sdnn_fail(SDNN_EHIP, "launch: %s", hipGetErrorString(e));
+}
+// d_packed of a call; sdnn_pack.hip
+int sdnn_check_pack8(const void *d_packed, size_t packed_bytes, int32_t n, int32_t B, float cap);

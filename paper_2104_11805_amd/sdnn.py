@@ -51,7 +51,18 @@ SIGNATURES = {
     "sdnn_forward_noalloc": (C.c_int, [_P, _P, _I32, _P, _P]),
     "sdnn_forward_skip_dead": (C.c_int, [_P, _P, _I32, _P, _I32, _P, _P]),
     "sdnn_backward": (C.c_int, [_P, _P, _P]),
+    "sdnn_backward_input": (C.c_int, [_P, _P, _P, _P]),
     "sdnn_sgd_step": (C.c_int, [_P, C.c_float, _P]),
+    "sdnn_pack8_bytes": (C.c_int, [_I32, _I32, C.POINTER(_SZ)]),
+    "sdnn_pack8": (C.c_int, [_P, _I32, _I32, C.c_float, _P, _SZ, _P]),
+    "sdnn_unpack8": (C.c_int, [_P, _SZ, _I32, _I32, C.c_float, _P, _P]),
+    "sdnn_checkpoint_bytes": (C.c_int, [_P, _I32, C.POINTER(_SZ)]),
+    "sdnn_checkpoint_save": (C.c_int, [_P, _P, _SZ, _P]),
+    "sdnn_checkpoint_load": (C.c_int, [_P, _P, _SZ, _I32, _P]),
+    "sdnn_layernorm_workspace_bytes": (C.c_int, [_I32, _I32, C.POINTER(_SZ)]),
+    "sdnn_layernorm": (C.c_int, [_P, _P, _P, _I32, _I32, C.c_double, _P, _P, _P, _SZ, _P]),
+    "sdnn_layernorm_backward": (C.c_int, [_P, _P, _P, _P, _I32, _I32, _P, _P, _P, _P, _SZ, _P]),
+    "sdnn_layernorm_backward_packed": (C.c_int, [_P, _P, _SZ, C.c_float, _P, _P, _I32, _I32, _P, _P, _P, _P, _SZ, _P]),
     "sdnn_get_activation": (C.c_int, [_P, _I32, _P, _P]),
     "sdnn_get_delta": (C.c_int, [_P, _I32, _P, _P]),
     "sdnn_weight_grad": (C.c_int, [_P, _I32, _P, _P, _P]),
@@ -165,6 +176,52 @@ def _dp(t):
     return C.c_void_p(t.data_ptr())
 
 
+def _tensor(t, name, shape, dtype, device, least=False):
+    """Checks a device tensor of a call on blocks: its shape (least: at least that many elements), type, device and layout."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
+        raise SdnnError(SDNN_EINVAL, f"{name} must be a tensor on {device}")
+    if t.dtype != dtype:
+        raise SdnnError(SDNN_EINVAL, f"{name} must be {dtype}, not {t.dtype}")
+    if not t.is_contiguous():
+        raise SdnnError(SDNN_EINVAL, f"{name} must be contiguous")
+    if t.numel() < shape[0] if least else tuple(t.shape) != tuple(shape):
+        raise SdnnError(SDNN_EINVAL, f"{name} has shape {tuple(t.shape)}, {tuple(shape)} {'at least ' if least else ''}is wanted")
+    return t
+
+
+class _On:
+    """The device of a call's tensors as the current one, and the stream of the call as the current one, for what the call
+    allocates and launches."""
+
+    def __init__(self, device, stream):
+        import torch
+        self.device = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
+        self.stream = None if stream is None else torch.cuda.stream(stream)
+
+    def __enter__(self):
+        if self.device is not None:
+            self.device.__enter__()
+        if self.stream is not None:
+            self.stream.__enter__()
+        return _stream_ptr()
+
+    def __exit__(self, *exc):
+        if self.stream is not None:
+            self.stream.__exit__(*exc)
+        if self.device is not None:
+            self.device.__exit__(*exc)
+
+
+def _block(t, name):
+    """[n][B] of a block of fp32 on the GPU."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+        raise SdnnError(SDNN_EINVAL, f"{name} must be a two-dimensional tensor on the GPU")
+    _tensor(t, name, t.shape, torch.float32, t.device)
+    return t.shape
+
+
 class Net:
     """Owns the workspace tensor and the opaque sdnn_net handle."""
 
@@ -237,8 +294,41 @@ class Net:
     def sdnn_backward(self, dloss, stream=None):
         _check(lib().sdnn_backward(self._handle, _dp(dloss), _stream_ptr(stream)), self._handle)
 
+    def sdnn_backward_input(self, dloss, dx0=None, stream=None):
+        """sdnn_backward that also forms dJ/dX_0 [n_in(1)][B], in dx0 if it is given."""
+        import torch
+        _tensor(dloss, "dloss", (self.shapes[-1][0], _block(dloss, "dloss")[1]), torch.float32, self.device)
+        shape = (self.shapes[0][1], dloss.shape[1])
+        with _On(self.device, stream) as s:
+            dx0 = self._empty(*shape) if dx0 is None else _tensor(dx0, "dx0", shape, torch.float32, self.device)
+            _check(lib().sdnn_backward_input(self._handle, _dp(dloss), _dp(dx0), s), self._handle)
+        return dx0
+
     def sdnn_sgd_step(self, lr: float, stream=None):
         _check(lib().sdnn_sgd_step(self._handle, C.c_float(lr), _stream_ptr(stream)), self._handle)
+
+    # -- activations in 8 bits --
+    def sdnn_checkpoint_bytes(self, b: int) -> int:
+        n = C.c_size_t(0)
+        _check(lib().sdnn_checkpoint_bytes(self._handle, int(b), C.byref(n)))
+        return n.value
+
+    def sdnn_checkpoint_save(self, b: int, ckpt=None, stream=None):
+        """The activations of the forward pass of b samples that came last, in 8 bits (in ckpt, a uint8 tensor, if it is given)."""
+        import torch
+        nbytes = self.sdnn_checkpoint_bytes(b)
+        with _On(self.device, stream) as s:
+            if ckpt is None:
+                ckpt = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            _tensor(ckpt, "ckpt", (nbytes,), torch.uint8, self.device, least=True)
+            _check(lib().sdnn_checkpoint_save(self._handle, _dp(ckpt), ckpt.numel(), s), self._handle)
+        return ckpt
+
+    def sdnn_checkpoint_load(self, ckpt, b: int, stream=None):
+        import torch
+        _tensor(ckpt, "ckpt", (0,), torch.uint8, self.device, least=True)
+        with _On(self.device, stream) as s:
+            _check(lib().sdnn_checkpoint_load(self._handle, _dp(ckpt), ckpt.numel(), int(b), s), self._handle)
 
     # -- inspection --
     def _empty(self, *shape, dtype=None):
@@ -291,3 +381,102 @@ def sdnn_gather_probe(table, v: int, idx_i32, n_waves: int, per_wave: int, out, 
     """table [rows][64*v] fp32, idx int32 [n_waves*per_wave], out fp32 [n_waves*64]: all device tensors."""
     _check(lib().sdnn_gather_probe(_dp(table), table.shape[0], int(v), _dp(idx_i32), int(n_waves), int(per_wave), _dp(out),
                                    _stream_ptr(stream)))
+
+
+# ---- blocks: activations in 8 bits, layer norm -------------------------------------
+
+def sdnn_pack8_bytes(n: int, b: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().sdnn_pack8_bytes(int(n), int(b), C.byref(nbytes)))
+    return nbytes.value
+
+
+class Packed8:
+    """A block [n][b] in 8 bits: its bytes (a uint8 tensor) and the cap that they were made with (0: values of both signs)."""
+
+    def __init__(self, data, n: int, b: int, cap: float = 0.0):
+        self.data, self.n, self.b, self.cap = data, int(n), int(b), float(cap)
+
+
+def sdnn_pack8(x, cap: float = 0.0, packed=None, stream=None) -> Packed8:
+    """packed: a uint8 tensor of sdnn_pack8_bytes, or None."""
+    import torch
+    n, b = _block(x, "x")
+    nbytes = sdnn_pack8_bytes(n, b)
+    with _On(x.device, stream) as s:
+        if packed is None:
+            packed = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+        _tensor(packed, "packed", (nbytes,), torch.uint8, x.device, least=True)
+        _check(lib().sdnn_pack8(_dp(x), n, b, cap, _dp(packed), packed.numel(), s))
+    return Packed8(packed, n, b, cap)
+
+
+def sdnn_unpack8(packed: Packed8, x=None, stream=None):
+    import torch
+    data = packed.data
+    _tensor(data, "packed.data", (0,), torch.uint8, data.device, least=True)
+    with _On(data.device, stream) as s:
+        if x is None:
+            x = torch.empty(packed.n, packed.b, device=data.device)
+        _tensor(x, "x", (packed.n, packed.b), torch.float32, data.device)
+        _check(lib().sdnn_unpack8(_dp(data), data.numel(), packed.n, packed.b, packed.cap, _dp(x), s))
+    return x
+
+
+def sdnn_layernorm_workspace_bytes(n: int, b: int) -> int:
+    nbytes = C.c_size_t(0)
+    _check(lib().sdnn_layernorm_workspace_bytes(int(n), int(b), C.byref(nbytes)))
+    return nbytes.value
+
+
+def _work(work, n, b, device):
+    import torch
+    nbytes = sdnn_layernorm_workspace_bytes(n, b)
+    if work is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _tensor(work, "work", (nbytes,), torch.uint8, device, least=True)
+
+
+def sdnn_layernorm(x, gamma=None, beta=None, eps: float = 1e-5, y=None, stats=None, work=None, stream=None):
+    """(y, stats): the block x [n][B] normalized over its rows, and what the backward pass reads, float64 [2][B]."""
+    import torch
+    n, b = _block(x, "x")
+    for t, name in ((gamma, "gamma"), (beta, "beta")):
+        if t is not None:
+            _tensor(t, name, (n,), torch.float32, x.device)
+    with _On(x.device, stream) as s:
+        work = _work(work, n, b, x.device)
+        y = torch.empty_like(x) if y is None else _tensor(y, "y", (n, b), torch.float32, x.device)
+        if stats is None:
+            stats = torch.empty(2, b, dtype=torch.float64, device=x.device)
+        _tensor(stats, "stats", (2, b), torch.float64, x.device)
+        _check(lib().sdnn_layernorm(_dp(x), _dp(gamma), _dp(beta), n, b, eps, _dp(y), _dp(stats), _dp(work), work.numel(), s))
+    return y, stats
+
+
+def sdnn_layernorm_backward(dy, x, stats, gamma=None, dx=None, dgamma=None, dbeta=None, work=None, stream=None):
+    """(dx, dgamma, dbeta).  x: the block that was normalized, or a Packed8 of it; stats: of the forward pass."""
+    import torch
+    n, b = _block(dy, "dy")
+    dev = dy.device
+    packed = isinstance(x, Packed8)
+    if packed:
+        if (x.n, x.b) != (n, b):
+            raise SdnnError(SDNN_EINVAL, f"x has {x.n} x {x.b} values, dy {n} x {b}")
+        _tensor(x.data, "x.data", (0,), torch.uint8, dev, least=True)
+    else:
+        _tensor(x, "x", (n, b), torch.float32, dev)
+    _tensor(stats, "stats", (2, b), torch.float64, dev)
+    if gamma is not None:
+        _tensor(gamma, "gamma", (n,), torch.float32, dev)
+    with _On(dev, stream) as s:
+        work = _work(work, n, b, dev)
+        dx = torch.empty_like(dy) if dx is None else _tensor(dx, "dx", (n, b), torch.float32, dev)
+        dgamma = torch.empty(n, device=dev) if dgamma is None else _tensor(dgamma, "dgamma", (n,), torch.float32, dev)
+        dbeta = torch.empty(n, device=dev) if dbeta is None else _tensor(dbeta, "dbeta", (n,), torch.float32, dev)
+        out = (n, b, _dp(dx), _dp(dgamma), _dp(dbeta), _dp(work), work.numel(), s)
+        if packed:
+            _check(lib().sdnn_layernorm_backward_packed(_dp(dy), _dp(x.data), x.data.numel(), x.cap, _dp(stats), _dp(gamma), *out))
+        else:
+            _check(lib().sdnn_layernorm_backward(_dp(dy), _dp(x), _dp(stats), _dp(gamma), *out))
+    return dx, dgamma, dbeta
