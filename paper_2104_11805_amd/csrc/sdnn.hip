@@ -135,7 +135,13 @@ __device__ __forceinline__ float act_backprop(int act, double value, float x, fl
         const double xd = (double)x;
         return (float)(value * (xd * (1.0 - xd)));
     }
-    return (x > 0.0f && x < capf) || act == ACT_NONE ? (float)value : 0.0f;
+    return (x > 0.0f && x < capf) ? (float)value : 0.0f;
+}
+
+// The same where the result may be dJ/dX_0 (ACT at compile time, act at run time).
+template <int ACT> __device__ __forceinline__ float act_backprop_to(int act, double value, float x, float capf)
+{
+    return ACT == ACT_NONE ? (float)value : act_backprop(act, value, x, capf);
 }
 
 // Orders the LDS (or in-place global) accesses of the lanes of one wavefront: what the lanes wrote before
@@ -214,7 +220,6 @@ struct GradArgs : SpmmArgs {
     float *g_part[2];  // gradient of the stored entries over the samples of the first / second tile, in the order of the
                        // transposed index [nnz]
     int32_t store_out; // 0 = only the gradient is wanted (first layer: there is no Delta_0)
-    int32_t ld_dst;    // floats per row of `out` (ld_out: of X_{l-1})
 };
 static_assert(sizeof(SpmmArgs) == 128, "see above");
 
@@ -388,7 +393,7 @@ __device__ __forceinline__ void spmm_row(RowMeta m, const int32_t *idx, const fl
         for (int v = 0; v < V; ++v) o[v] = act_apply(ACT, acc[v] + b, capf); // compile-time: exp() costs registers
     } else {
 #pragma unroll
-        for (int v = 0; v < V; ++v) o[v] = act_backprop(act, acc[v], xp[v], capf);
+        for (int v = 0; v < V; ++v) o[v] = act_backprop_to<ACT>(act, acc[v], xp[v], capf);
     }
     if (V > 1 && s + V > B) { // the batch's last piece
 #pragma unroll
@@ -648,21 +653,16 @@ __device__ __forceinline__ float add_neighbour16(float g)
     return (float)((double)__uint_as_float(t[0]) + (double)__uint_as_float(t[1]));
 }
 
-// Four samples of a row of Delta_{l-1}, or of dJ/dX_0 in the caller's rows of B floats; zeros after the batch's last sample.
-__device__ __forceinline__ void store_group(const GradArgs &a, int row, int s, float (&o)[4])
+// Four samples of a row of dJ/dX_0, in the caller's rows of B floats.
+__device__ __forceinline__ void store_input(const GradArgs &a, int row, int s, const double (&acc)[4])
 {
-    float *dst = a.out + (size_t)row * a.ld_dst + s;
-    if (((a.ld_dst & 3) | ((int)(size_t)a.out & 15)) == 0) {
-        if (s + 4 > a.B) { // the batch's last group
-#pragma unroll
-            for (int v = 1; v < 4; ++v)
-                if (s + v >= a.B) o[v] = 0.0f;
-        }
-        stv<4>(dst, o);
+    float *dst = a.out + (size_t)row * a.B + s;
+    if (((a.B & 3) | ((int)(size_t)a.out & 15)) == 0) {
+        *reinterpret_cast<float4 *>(dst) = make_float4((float)acc[0], (float)acc[1], (float)acc[2], (float)acc[3]);
     } else {
 #pragma unroll
         for (int v = 0; v < 4; ++v)
-            if (s + v < a.B) dst[v] = o[v];
+            if (s + v < a.B) dst[v] = (float)acc[v];
     }
 }
 
@@ -676,8 +676,9 @@ __device__ __forceinline__ void store_group(const GradArgs &a, int row, int s, f
 // 14.4 (64), 31.8 -> 25.3 (128; two launches on two streams before); 10007 neurons, 99 samples 32.5 (two
 // separate kernels) -> 17.6 + 3; 8192 neurons of 820 entries 420 -> 331 (256 samples), 410 -> 127 (64).
 // TWO (G = 32, 128 samples): the gradient is the sum of two windows of 64 samples, each rounded to fp32 (two_windows).
-template <int G, bool TWO>
-__global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_rows(const GradArgs a)
+// INPUT (first layer): W_1^T Delta_1 goes to the caller as it is.
+template <int G, bool TWO, bool INPUT>
+__device__ __forceinline__ void bwd_rows(const GradArgs &a)
 {
     static_assert(!TWO || G == 32, "two windows of 16 lanes");
     constexpr int R = 64 / G;
@@ -746,11 +747,23 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_rows(const GradArgs a)
         consume(x1, w1);
     }
     if (!a.store_out || !live) return;
+    if constexpr (INPUT) {
+        store_input(a, row, s, acc);
+        return;
+    }
     float o[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) o[v] = act_backprop(a.act, acc[v], xp[v], a.cap);
-    store_group(a, row, s, o);
+    if (s + 4 > a.B) { // the batch's last group
+#pragma unroll
+        for (int v = 1; v < 4; ++v)
+            if (s + v >= a.B) o[v] = 0.0f;
+    }
+    stv<4>(a.out + (size_t)row * a.ld_out + s, o);
 }
+
+template <int G, bool TWO> __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_rows(const GradArgs a) { bwd_rows<G, TWO, false>(a); }
+template <int G, bool TWO> __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_rows_input(const GradArgs a) { bwd_rows<G, TWO, true>(a); }
 
 // The same sweep for long rows and more than 128 samples: a wavefront per row.  k_bwd_rows<64> keeps the vector units issuing in
 // 91 % of its clocks there (23 instructions per entry, 6.5 of them the sum over the lanes, 3 to hand the entries round).  Here a
@@ -764,7 +777,8 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_rows(const GradArgs a)
 // a stream of such gathers alone reaches 26 to 31.  (Eight to sixteen gathers in flight, four or five wavefronts per SIMD: the same.)
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-__global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_long(const GradArgs a)
+template <bool INPUT>
+__device__ __forceinline__ void bwd_long_rows(const GradArgs a)
 {
     typedef const int __attribute__((address_space(4))) *int_ptr;
     typedef const float __attribute__((address_space(4))) *float_ptr;
@@ -866,11 +880,22 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_long(const GradArgs a)
         w = wn;
     }
     if (!a.store_out || !live) return;
+    if constexpr (INPUT) {
+        store_input(a, row, s, acc);
+        return;
+    }
     float o[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) o[v] = act_backprop(a.act, acc[v], xp[v], a.cap);
-    store_group(a, row, s, o);
+    if (s + 4 > a.B) { // the batch's last group
+#pragma unroll
+        for (int v = 1; v < 4; ++v)
+            if (s + v >= a.B) o[v] = 0.0f;
+    }
+    stv<4>(a.out + (size_t)row * a.ld_out + s, o);
 }
+__global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_long(const GradArgs a) { bwd_long_rows<false>(a); }
+__global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_long_input(const GradArgs a) { bwd_long_rows<true>(a); }
 
 // ---------------------------------------------------------------------------
 // K1p / K2p: the same product for wide layers with short rows, swept in column panels.
@@ -1000,7 +1025,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_spmm_panel(const SpmmArgs a, 
             if (row[r] < 0) continue;
             float o;
             if (MODE == 0) o = act_apply(ACT, acc[r] + (a.aux ? (double)a.aux[row[r]] : 0.0), a.cap);
-            else o = act_backprop(a.act, acc[r], xp[r], a.cap);
+            else o = act_backprop_to<ACT>(a.act, acc[r], xp[r], a.cap);
             if (live) a.out[(size_t)row[r] * ld + s] = o;
         }
         if (fills_up(B, a.ld_out) && is_fill(s_own, B)) {
@@ -2103,7 +2128,7 @@ __global__ void __launch_bounds__(256) k_pan_turn(float *__restrict__ x, int ld,
 #define TR_SPAN 8192   // consecutive entries of the transposed index that one workgroup of k_apply takes (32 KiB of LDS)
 #define GRAD_LD 68 // floats per parked entry: 64 samples + pad (rows stay 16-byte aligned, banks spread)
 #define GRAD_GE 16 // entries parked at a time: 4.6 KB of LDS per wavefront, which keeps 8 wavefronts per SIMD
-template <int U>
+template <int U, bool INPUT>
 __device__ __forceinline__ void spmm_row_grad(RowMeta m, const GradArgs &a, int lane,
                                               float *__restrict__ dt, float *__restrict__ xt)
 {
@@ -2180,10 +2205,13 @@ __device__ __forceinline__ void spmm_row_grad(RowMeta m, const GradArgs &a, int 
             wave_lds_sync(); // the next group's rows are parked over the ones just read
         }
     }
-    if (a.store_out && lane < (fills_up(B, a.ld_dst) ? (B + 3) & ~3 : B))
-        a.out[(size_t)m.row * a.ld_dst + lane] = live ? act_backprop(a.act, acc, xp, a.cap) : 0.0f;
+    if (INPUT) {
+        if (live) a.out[(size_t)m.row * B + lane] = (float)acc;
+    } else if (a.store_out && lane < (fills_up(B, a.ld_out) ? (B + 3) & ~3 : B)) {
+        a.out[(size_t)m.row * ld + lane] = live ? act_backprop(a.act, acc, xp, a.cap) : 0.0f;
+    }
 }
-template <int U>
+template <int U, bool INPUT>
 __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_grad(const GradArgs a)
 {
     __shared__ __attribute__((aligned(16))) float dt[WAVES_PER_BLOCK][GRAD_GE * GRAD_LD];
@@ -2194,7 +2222,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_bwd_grad(const GradArgs a)
         const int r = __builtin_amdgcn_readfirstlane((int)(vb * WAVES_PER_BLOCK + wave));
         if (r >= a.n_rows) continue;
         const RowMeta m = load_meta<0>(a.sched, a.idx, a.vals, nullptr, r, lane);
-        spmm_row_grad<U>(m, a, lane, dt[wave], xt[wave]);
+        spmm_row_grad<U, INPUT>(m, a, lane, dt[wave], xt[wave]);
     }
 }
 
@@ -2258,7 +2286,7 @@ __global__ void __launch_bounds__(256) k_spmv(const SpmmArgs a)
             if (p0 + k < end) acc = fma((double)w[k], (double)x[k], acc);
     }
     if (MODE == 0) a.out[row] = act_apply(a.act, acc + (a.aux ? (double)a.aux[row] : 0.0), a.cap);
-    else a.out[row] = act_backprop(a.act, acc, a.aux[row], a.cap);
+    else a.out[row] = a.act == ACT_NONE ? (float)acc : act_backprop(a.act, acc, a.aux[row], a.cap);
 }
 
 // Same product for narrow layers, where a lane per row leaves most of the chip idle: a wavefront
@@ -2289,7 +2317,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_spmv_wave(const SpmmArgs a)
     }
     if (lane == 0) {
         if (MODE == 0) a.out[row] = act_apply(a.act, acc + (a.aux ? (double)a.aux[row] : 0.0), a.cap);
-        else a.out[row] = act_backprop(a.act, acc, a.aux[row], a.cap);
+        else a.out[row] = a.act == ACT_NONE ? (float)acc : act_backprop(a.act, acc, a.aux[row], a.cap);
     }
 }
 
@@ -2356,7 +2384,7 @@ __global__ void __launch_bounds__(64) k_spmv_stage(const SpmmArgs a, int R)
     }
     if (lane < nr) {
         if (MODE == 0) a.out[row] = act_apply(a.act, acc + (a.aux ? (double)a.aux[row] : 0.0), a.cap);
-        else a.out[row] = act_backprop(a.act, acc, a.aux[row], a.cap);
+        else a.out[row] = a.act == ACT_NONE ? (float)acc : act_backprop(a.act, acc, a.aux[row], a.cap);
     }
 }
 
@@ -2384,7 +2412,7 @@ struct SpmvLmArgs {
     unsigned lm_bytes;
     const float *in;
     unsigned in_bytes;
-    const float *aux;    // MODE 0: biases, MODE 1 and 2: X_{l-1}; in the order of the results' places
+    const float *aux;    // MODE 0: biases, MODE 1 and 2: X_{l-1}; in the order of the results' places (MODE 3, dJ/dX_0: NULL)
     float *out;
     float cap;
     int32_t act;
@@ -2467,7 +2495,7 @@ __global__ void __launch_bounds__(64) k_spmv_lm(const SpmvLmArgs a)
     }
     if (dst < 0) return;
     if (MODE == 0) a.out[dst] = act_apply(a.act, acc + (double)aux, a.cap);
-    else a.out[dst] = act_backprop(a.act, acc, aux, a.cap);
+    else a.out[dst] = MODE == 3 ? (float)acc : act_backprop(a.act, acc, aux, a.cap);
 }
 
 // The step of such a net: w -= lr (delta_j x_i) on both copies, in a stream over each; the lane's own row gives one of the
@@ -4443,11 +4471,12 @@ static int pick_v_spmm(int B, int ld_in, int ld_out, const void *in, const void 
     return 1;
 }
 
-// Kernel tables.  The forward kernels are compiled per activation, the backward ones once (ACT = 0).
+// Kernel tables.  The forward kernels are compiled per activation, the backward ones once (ACT = 0), and for dJ/dX_0 (ACT_NONE).
 template <int MODE, int V, int U, bool TI>
 static const void *spmm_fn_act(int act)
 {
     if (MODE == 0 && act == ACT_SIGMOID) return (const void *)k_spmm<V, MODE, U, TI, (MODE == 0 ? ACT_SIGMOID : 0)>;
+    if (MODE == 1 && act == ACT_NONE) return (const void *)k_spmm<V, MODE, U, TI, (MODE == 1 ? ACT_NONE : 0)>;
     return (const void *)k_spmm<V, MODE, U, TI, 0>;
 }
 template <int MODE, int V>
@@ -4466,6 +4495,7 @@ template <int MODE, int R>
 static const void *panel_fn_act(int act)
 {
     if (MODE == 0 && act == ACT_SIGMOID) return (const void *)k_spmm_panel<R, MODE, (MODE == 0 ? ACT_SIGMOID : 0)>;
+    if (MODE == 1 && act == ACT_NONE) return (const void *)k_spmm_panel<R, MODE, (MODE == 1 ? ACT_NONE : 0)>;
     return (const void *)k_spmm_panel<R, MODE, 0>;
 }
 template <int MODE>
@@ -4500,7 +4530,7 @@ static int launch_spmm_panel(sdnn_net *net, const LayerDev &d, SpmmArgs a, int B
         if (ri == 3) break;
     }
     const int R = 1 << ri;
-    const void *fn = panel_fn<MODE>(ri, net->cfg.activation);
+    const void *fn = panel_fn<MODE>(ri, a.act);
     a.n_rg = (uint32_t)((a.n_rows + WAVES_PER_BLOCK * R - 1) / (WAVES_PER_BLOCK * R));
     const uint64_t blocks = (uint64_t)a.n_tiles * a.n_rg;
     if (blocks > 0x7fffffffull) return fail(net, SDNN_EINVAL, "grid too large");
@@ -4582,7 +4612,10 @@ static int launch_spmm(sdnn_net *net, const LayerDev &d, const float *in, int ld
         b.cs = d.b1_cs[o]; b.row = d.b1_row[o]; b.lm = (const uint4 *)d.b1_lm[o]; b.in = in; b.in_bytes = a.in_bytes; b.aux = aux; b.out = out;
         b.lm_bytes = 0xffffffffu; // every chunk that the table names is there
         b.cap = a.cap; b.act = a.act;
-        if (net->b1_wide) hipLaunchKernelGGL((k_spmv_lm<MODE, true, true>), dim3((unsigned)d.b1_blocks[o]), dim3(64), 0, stream, b);
+        if (act == ACT_NONE) b.aux = nullptr;
+        if (MODE == 1 && act == ACT_NONE && net->b1_wide) hipLaunchKernelGGL((k_spmv_lm<3 * MODE, true, true>), dim3((unsigned)d.b1_blocks[o]), dim3(64), 0, stream, b);
+        else if (MODE == 1 && act == ACT_NONE) hipLaunchKernelGGL((k_spmv_lm<3 * MODE, false, true>), dim3((unsigned)d.b1_blocks[o]), dim3(64), 0, stream, b);
+        else if (net->b1_wide) hipLaunchKernelGGL((k_spmv_lm<MODE, true, true>), dim3((unsigned)d.b1_blocks[o]), dim3(64), 0, stream, b);
         else if (MODE == 1 && d.b1_blocks[o] > 3 * net->n_cu)
             hipLaunchKernelGGL((k_spmv_lm<2 * MODE, false, true>), dim3((unsigned)d.b1_blocks[o]), dim3(64), 0, stream, b);
         else hipLaunchKernelGGL((k_spmv_lm<MODE, false, true>), dim3((unsigned)d.b1_blocks[o]), dim3(64), 0, stream, b);
@@ -4658,11 +4691,11 @@ static int launch_spmm(sdnn_net *net, const LayerDev &d, const float *in, int ld
     const bool tiles_inner = !long_rows && a.n_tiles >= 2 && a.n_tiles < 8;
     if (tiles_inner) g = a.n_rg;
     const int U = long_rows ? 16 : 8;
-    const void *fn = spmm_fn<MODE>(V, U, tiles_inner, net->cfg.activation);
+    const void *fn = spmm_fn<MODE>(V, U, tiles_inner, act);
     if (!long_rows) {
         int &per_cu = net->occ_spmm[MODE][V == 4 ? 2 : V == 2 ? 1 : 0][tiles_inner ? 1 : 0][U == 16 ? 1 : 0];
         if (per_cu == 0) {
-            HIP_TRY(net, hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, fn, BLOCK_THREADS, 0));
+            HIP_TRY(net, hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, spmm_fn<MODE>(V, U, tiles_inner, net->cfg.activation), BLOCK_THREADS, 0));
             if (per_cu < 1) per_cu = 1;
         }
         g = std::min(g, (uint64_t)per_cu * (uint64_t)net->n_cu);
@@ -5221,17 +5254,21 @@ static int launch_input_grad(sdnn_net *net, float *out, hipStream_t stream)
     return launch_spmm<1>(net, d, d.D, net->ld, out, net->B, out, net->B, stream, nullptr, nullptr, 0, 0, ACT_NONE);
 }
 
+template <int G, bool TWO> static const void *rows_grad_fn(bool input)
+{
+    return input ? (const void *)k_bwd_rows_input<G, TWO> : (const void *)k_bwd_rows<G, TWO>;
+}
 // Fused back-propagation + entry gradient of one layer.  out NULL, for the first layer: gradient only, there is no Delta_0;
 // else for the first layer the caller's dJ/dX_0.
 static int launch_bwd_grad(sdnn_net *net, const LayerDev &d, float *out, hipStream_t stream)
 {
-    const bool first = &d == net->layers.data();
+    const bool first = &d == net->layers.data(), input = first && out;
     const int B = net->Bp;
     GradArgs a;
     a.row_ptr = d.t_row_ptr; a.idx = d.t_row_idx; a.perm = nullptr; a.sched = d.t_sched; a.n_rows = d.n_in;
     a.vals = d.vals_t; a.in = d.D; a.out = out; a.aux = d.X_prev; a.B = net->B; a.ld_in = a.ld_out = net->ld; a.cap = net->cfg.act_cap;
-    a.act = first ? ACT_NONE : net->cfg.activation; a.n_live = nullptr; a.flags = nullptr;
-    a.g_part[0] = d.G[0]; a.g_part[1] = d.G[1]; a.store_out = out ? 1 : 0; a.ld_dst = first ? net->B : net->ld;
+    a.act = net->cfg.activation; a.n_live = nullptr; a.flags = nullptr;
+    a.g_part[0] = d.G[0]; a.g_part[1] = d.G[1]; a.store_out = out ? 1 : 0;
     if (a.n_rows == 0 || d.nnz == 0) {
         if (d.nnz == 0 && out && a.n_rows > 0) // no entries: Delta_{l-1} = 0, nothing to differentiate
             return first ? launch_input_grad(net, out, stream) : launch_spmm<1>(net, d, d.D, net->ld, out, net->ld, d.X_prev, net->B, stream);
@@ -5247,9 +5284,9 @@ static int launch_bwd_grad(sdnn_net *net, const LayerDev &d, float *out, hipStre
     if (B <= 64 && ((a.n_rows <= 6144 && (int64_t)d.nnz < 128 * (int64_t)a.n_rows) || !wide_rows(net, d))) {
         // few short rows: a wavefront for each keeps more of the chip busy than several rows per wavefront (4096 rows, 64
         // samples: 7.3 vs 8.2 us; 6500 rows: 9.9 vs 9.0)
-        const void *fn = (const void *)k_bwd_grad<8>;
+        const void *fn = input ? (const void *)k_bwd_grad<8, true> : (const void *)k_bwd_grad<8, false>;
         if (net->occ_grad == 0) {
-            HIP_TRY(net, hipOccupancyMaxActiveBlocksPerMultiprocessor(&net->occ_grad, fn, BLOCK_THREADS, 0));
+            HIP_TRY(net, hipOccupancyMaxActiveBlocksPerMultiprocessor(&net->occ_grad, (const void *)k_bwd_grad<8, false>, BLOCK_THREADS, 0));
             if (net->occ_grad < 1) net->occ_grad = 1;
         }
         uint64_t g = std::min<uint64_t>(a.n_vblocks, (uint64_t)net->occ_grad * (uint64_t)net->n_cu);
@@ -5265,10 +5302,13 @@ static int launch_bwd_grad(sdnn_net *net, const LayerDev &d, float *out, hipStre
     const int rows_per_block = 64 / G * WAVES_PER_BLOCK;
     a.n_tiles = (uint32_t)net->grad_parts;
     a.n_rg = (uint32_t)((a.n_rows + rows_per_block - 1) / rows_per_block);
-    const void *fn = G == 4 ? (const void *)k_bwd_rows<4, false> : G == 8 ? (const void *)k_bwd_rows<8, false>
-                     : G == 16 ? (const void *)k_bwd_rows<16, false>
-                     : G == 64 ? (bwd_long(d, a.in_bytes, B) ? (const void *)k_bwd_long : (const void *)k_bwd_rows<64, false>)
-                     : two ? (const void *)k_bwd_rows<32, true> : (const void *)k_bwd_rows<32, false>;
+    const bool by_long = G == 64 && bwd_long(d, a.in_bytes, B);
+    const void *fn = by_long   ? input ? (const void *)k_bwd_long_input : (const void *)k_bwd_long
+                     : G == 4  ? rows_grad_fn<4, false>(input)
+                     : G == 8  ? rows_grad_fn<8, false>(input)
+                     : G == 16 ? rows_grad_fn<16, false>(input)
+                     : G == 64 ? rows_grad_fn<64, false>(input)
+                     : two     ? rows_grad_fn<32, true>(input) : rows_grad_fn<32, false>(input);
     HIP_TRY(net, hipLaunchKernel(fn, dim3(a.n_tiles * a.n_rg), dim3(BLOCK_THREADS), args, 0, stream));
     HIP_TRY(net, hipGetLastError());
     return SDNN_OK;
