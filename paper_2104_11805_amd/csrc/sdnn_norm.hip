@@ -1,278 +1,475 @@
 // Layer norm over the neurons of each sample, forward and backward, on blocks [n][B].
 //
-// Two launches each: sums over the rows of a range per workgroup, then every workgroup adds up the ranges' sums for its columns and
-// writes its part of the result.  Sums are fp64 and in a fixed order.
+// The sums of a sample run down a column of the block, those of gamma's and beta's gradients along a row.  Two launches each, over
+// tiles of CL * 4 columns and a range of rows: the first leaves every tile's sums over its rows (back: and over its columns), the
+// second adds up the sums of the tiles above and below (back: to the left and right) and writes the result.  A lane holds four
+// neighbouring columns, CL lanes lie across a tile, the others of a wavefront over the rows; NORM_ROWS rows per thread are requested
+// at a time.  Sums are fp64 and in a fixed order, a result is rounded once.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 #include <cmath>
 
 #include "sdnn_internal.h"
+#include "sdnn_lanes.h"
 #include "sdnn_pack8.h"
 
-#define NORM_THREADS 256
+#define NORM_THREADS 512
+#define NORM_ROWS 4
+
+struct __attribute__((packed, aligned(4))) F4 { float v[4]; }; // 16 bytes at any multiple of 4
+struct __attribute__((packed, aligned(1))) U1 { unsigned v; }; // 4 bytes anywhere
+
+// A lane's four columns.  They end with the block's last column at the latest: the last lane's first ones may be its neighbour's, and
+// are left out of everything.  SMALL: B < 4, one lane across.
+template <int CL, bool SMALL> struct Columns {
+    static constexpr bool small = SMALL;
+    int tile0, base, first, B; // columns base .. base + 3, of which those from `first` on are the lane's own; none if first >= B
+    __device__ __forceinline__ Columns(int tile, int B_)
+    {
+        B = B_;
+        tile0 = tile * 4 * CL;
+        first = tile0 + 4 * (int)(threadIdx.x & (CL - 1));
+        base = SMALL ? 0 : min(first, B - 4);
+    }
+    __device__ __forceinline__ bool any() const { return first < B; }
+    __device__ __forceinline__ bool whole() const { return !SMALL && base == first; }
+    __device__ __forceinline__ bool own(int v) const { return SMALL ? v < B : base + v >= first; }
+    __device__ __forceinline__ bool ragged() const { return SMALL || tile0 + 4 * CL > B; } // some lane of the tile is not whole (uniform)
+};
 
 // The block that is normalized, as it is ...
 struct PlainBlock {
     const float *x;
-    template <int V> __device__ __forceinline__ void load(size_t e, float (&v)[V]) const
+    struct Raw { float v[4]; };
+    template <class C> __device__ __forceinline__ void request(const C &c, size_t row, Raw &t) const
     {
-        if constexpr (V == 4) {
-            const float4 t = *reinterpret_cast<const float4 *>(x + e);
-            v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
+        const float *p = x + row * (size_t)c.B + c.base;
+        if constexpr (C::small) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) t.v[v] = v < c.B ? p[v] : 0.0f;
         } else {
-            v[0] = x[e];
+            const F4 f = *reinterpret_cast<const F4 *>(p);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) t.v[v] = f.v[v];
         }
     }
+    __device__ __forceinline__ void values(const Raw &t, float (&x4)[4]) const
+    {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x4[v] = t.v[v];
+    }
 };
-// ... or in 8 bits
+// ... or in 8 bits: four codes, and the scales of the first and the last of them
 struct PackedBlock {
     const uint8_t *codes;
     const uint16_t *scales;
     float cap, below;
-    template <int V> __device__ __forceinline__ void load(size_t e, float (&v)[V]) const
+    struct Raw { unsigned code; float scale[2]; int place; };
+    template <class C> __device__ __forceinline__ void request(const C &c, size_t row, Raw &t) const
     {
-        const float t = __uint_as_float((unsigned)scales[e / PACK_GROUP] << 16);
-        if constexpr (V == 4) {
-            const unsigned c = *reinterpret_cast<const unsigned *>(codes + e);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = pack8_value(c >> (8 * k) & 255u, t, cap, below);
+        const size_t e = row * (size_t)c.B + c.base;
+        const int last = C::small ? c.B - 1 : 3;
+        if constexpr (C::small) {
+            t.code = codes[e];
+            for (int v = 1; v <= last; ++v) t.code |= (unsigned)codes[e + v] << (8 * v);
         } else {
-            v[0] = pack8_value(codes[e], t, cap, below);
+            t.code = reinterpret_cast<const U1 *>(codes + e)->v;
         }
+        t.place = (int)(e % PACK_GROUP);
+        t.scale[0] = __uint_as_float((unsigned)scales[e / PACK_GROUP] << 16);
+        t.scale[1] = __uint_as_float((unsigned)scales[(e + last) / PACK_GROUP] << 16);
+    }
+    __device__ __forceinline__ void values(const Raw &t, float (&x4)[4]) const
+    {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x4[v] = pack8_value(t.code >> (8 * v) & 255u, t.place + v < PACK_GROUP ? t.scale[0] : t.scale[1], cap, below);
     }
 };
 
-// A workgroup's threads: 1 << cl_log2 of them lie across the columns, V columns each, the others across the rows.
-struct Shape {
-    int32_t n, B, cl_log2, rows; // rows: of a range
+// The sum of a value over the lanes that hold the same columns, in all of them.
+template <int CL> __device__ __forceinline__ double add_rows(double v)
+{
+    if constexpr (CL <= 1) v += lane_xor<0>(v);
+    if constexpr (CL <= 2) v += lane_xor<1>(v);
+    if constexpr (CL <= 4) v += lane_xor<2>(v);
+    if constexpr (CL <= 8) v += lane_xor<3>(v);
+    if constexpr (CL <= 16) v = add_lane_xor<4>(v);
+    if constexpr (CL <= 32) v = add_lane_xor<5>(v);
+    return v;
+}
+
+// Stores the sums that the workgroup's threads have of their columns: part [B].
+template <int CL, class C>
+__device__ __forceinline__ void store_column_sums(const C &c, const double (&a)[4], const double (&b)[4], double2 *__restrict__ part)
+{
+    __shared__ double2 lds[NORM_THREADS / 64][4 * CL];
+    const int tid = threadIdx.x;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const double2 s = make_double2(add_rows<CL>(a[v]), add_rows<CL>(b[v]));
+        if ((tid & 63) < CL) lds[tid >> 6][4 * (tid & 63) + v] = s;
+    }
+    __syncthreads();
+    const int col = c.tile0 + tid;
+    if (tid < 4 * CL && col < c.B) {
+        const int slot = 4 * (tid >> 2) + (col - max(0, min(c.tile0 + 4 * (tid >> 2), c.B - 4)));
+        double2 s = lds[0][slot];
+        for (int w = 1; w < NORM_THREADS / 64; ++w) {
+            s.x += lds[w][slot].x;
+            s.y += lds[w][slot].y;
+        }
+        part[col] = s;
+    }
+}
+
+// The sums of all ranges for the tile's columns, put through `finish`; the results for the lane's columns.
+template <int CL, class C, class F>
+__device__ __forceinline__ void load_column_sums(const C &c, const double2 *__restrict__ part, int ranges, double (&a)[4], double (&b)[4], F finish)
+{
+    constexpr int CT = 4 * CL, K = NORM_THREADS / CT;
+    __shared__ double2 lds[NORM_THREADS];
+    const int tid = threadIdx.x, col = c.tile0 + (tid & (CT - 1));
+    double2 s = make_double2(0.0, 0.0);
+    if (col < c.B)
+#pragma unroll 4
+        for (int k = tid / CT; k < ranges; k += K) {
+            const double2 t = part[(size_t)k * c.B + col];
+            s.x += t.x;
+            s.y += t.y;
+        }
+    lds[tid] = s;
+    __syncthreads();
+    if (tid < CT) {
+        for (int k = 1; k < K; ++k) {
+            s.x += lds[k * CT + tid].x;
+            s.y += lds[k * CT + tid].y;
+        }
+        if (col < c.B) s = finish(col, s);
+        lds[tid] = s;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const double2 t = lds[max(0, min(c.base + v - c.tile0, CT - 1))];
+        a[v] = t.x;
+        b[v] = t.y;
+    }
+}
+
+// The rows that a thread walks: r0 + its place, in steps of NORM_THREADS / CL, NORM_ROWS of them at a time; body(row of each, how many of
+// them there are: NORM_ROWS but at a range's end).
+template <int CL, class F> __device__ __forceinline__ void walk_rows(int r0, int r1, F body)
+{
+    constexpr int STEP = NORM_THREADS / CL;
+    for (int r = r0 + (int)threadIdx.x / CL; r < r1; r += NORM_ROWS * STEP) {
+        const int left = (r1 - r + STEP - 1) / STEP;
+        if (left >= NORM_ROWS) body(r, std::integral_constant<bool, true>(), NORM_ROWS);
+        else body(r, std::integral_constant<bool, false>(), left);
+    }
+}
+
+struct NormArgs {
+    int32_t n, B, rows; // rows of a range
+    int32_t tiles, tile0, splits, ranges; // tiles of columns in this launch, the first of them; second launches: parts of a range, ranges
 };
 
-// Adds up V pairs of sums over the threads that share columns; afterwards the threads of the first row have them.
-template <int V> __device__ __forceinline__ void add_up(double (&a)[V], double (&b)[V], int cl_log2, double2 (*lds)[V])
+// part [range][B]: sums of x - x0 and of its square, x0 the sample's first value: nothing cancels where the mean is large.
+// firsts [B]: x0, which the second launch may write its results over.
+template <int CL, bool SMALL>
+__global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restrict__ x, const NormArgs a, double2 *__restrict__ part, float *__restrict__ firsts)
 {
-    const int tid = threadIdx.x, cl = 1 << cl_log2;
-    __syncthreads();
+    const int range = (int)blockIdx.x / a.tiles;
+    const Columns<CL, SMALL> c(a.tile0 + (int)blockIdx.x - range * a.tiles, a.B);
+    const int r0 = range * a.rows, r1 = min(a.n, r0 + a.rows);
+    const PlainBlock in{x};
+    double s1[4] = {}, s2[4] = {};
+    if (c.any()) {
+        PlainBlock::Raw first;
+        in.request(c, 0, first);
+        if (range == 0 && (int)threadIdx.x < CL)
 #pragma unroll
-    for (int v = 0; v < V; ++v) lds[tid][v] = make_double2(a[v], b[v]);
-    __syncthreads();
-    if (tid < cl)
-        for (int t = tid + cl; t < NORM_THREADS; t += cl)
+            for (int v = 0; v < 4; ++v)
+                if (c.own(v)) firsts[c.base + v] = first.v[v];
+        walk_rows<CL>(r0, r1, [&](int r, auto full, int left) {
+            PlainBlock::Raw t[NORM_ROWS];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                a[v] += lds[t][v].x;
-                b[v] += lds[t][v].y;
-            }
+            for (int u = 0; u < NORM_ROWS; ++u)
+                if (full.value || u < left) in.request(c, (size_t)r + u * (NORM_THREADS / CL), t[u]);
+#pragma unroll
+            for (int u = 0; u < NORM_ROWS; ++u)
+                if (full.value || u < left)
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const double d = (double)t[u].v[v] - (double)first.v[v];
+                        s1[v] += d;
+                        s2[v] = fma(d, d, s2[v]);
+                    }
+        });
+    }
+    store_column_sums<CL>(c, s1, s2, part + (size_t)range * a.B);
 }
 
-// part [range][B]: sums of x - x0 and of its square, x0 the sample's first value: no cancellation where the mean is large
-// (and firsts [B]: x0, which the second launch may write its results over)
-template <int V>
-__global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restrict__ x, Shape sh, double2 *__restrict__ part, float *__restrict__ firsts)
+// Which tile a workgroup of a second launch takes: the ranges of the first launch in `splits` parts, each on the XCD that has read it.
+__device__ __forceinline__ void second_tile(const NormArgs &a, int &tile, int &r0, int &r1)
 {
-    __shared__ double2 lds[NORM_THREADS][V];
-    const int col = ((int)(blockIdx.x << sh.cl_log2) + (int)(threadIdx.x & ((1 << sh.cl_log2) - 1))) * V;
-    const int r0 = (int)blockIdx.y * sh.rows, r1 = min(sh.n, r0 + sh.rows);
-    double s1[V] = {}, s2[V] = {};
-    if (col < sh.B) {
-        float first[V];
-        PlainBlock{x}.load<V>((size_t)col, first);
-        for (int r = r0 + (int)(threadIdx.x >> sh.cl_log2); r < r1; r += NORM_THREADS >> sh.cl_log2) {
-            float t[V];
-            PlainBlock{x}.load<V>((size_t)r * sh.B + col, t);
+    const unsigned all = (unsigned)a.tiles * (unsigned)a.ranges, whole = all & ~7u;
+    unsigned id, split;
+    if (blockIdx.x < whole * (unsigned)a.splits) {
+        const unsigned j = blockIdx.x >> 3;
+        id = 8 * (j / (unsigned)a.splits) + (blockIdx.x & 7);
+        split = j % (unsigned)a.splits;
+    } else {
+        const unsigned j = blockIdx.x - whole * (unsigned)a.splits;
+        id = whole + j / (unsigned)a.splits;
+        split = j % (unsigned)a.splits;
+    }
+    const int range = (int)(id / (unsigned)a.tiles), rows = (a.rows + a.splits - 1) / a.splits;
+    tile = a.tile0 + (int)(id % (unsigned)a.tiles);
+    r0 = min(a.n, range * a.rows + (int)split * rows);
+    r1 = min(min(a.n, (range + 1) * a.rows), r0 + rows);
+}
+
+template <class C> __device__ __forceinline__ void store_row(const C &c, float *p, const float (&o)[4])
+{
+    if (c.whole()) {
+        F4 f;
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const double d = (double)t[v] - (double)first[v];
-                s1[v] += d;
-                s2[v] = fma(d, d, s2[v]);
-            }
+        for (int v = 0; v < 4; ++v) f.v[v] = o[v];
+        *reinterpret_cast<F4 *>(p) = f;
+    } else {
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (c.own(v)) p[v] = o[v];
+    }
+}
+
+template <int CL, bool SMALL>
+__global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, const float *__restrict__ gamma, const float *__restrict__ beta, const NormArgs a,
+                                                             double eps, const double2 *__restrict__ part, const float *__restrict__ firsts, float *y,
+                                                             double *__restrict__ stats)
+{
+    int tile, r0, r1;
+    second_tile(a, tile, r0, r1);
+    const Columns<CL, SMALL> c(tile, a.B);
+    double mean[4], rstd[4];
+    const double inv = 1.0 / (double)a.n;
+    load_column_sums<CL>(c, part, a.ranges, mean, rstd, [&](int col, double2 s) {
+        const double m = s.x * inv, var = s.y * inv - m * m;
+        const double2 out = make_double2((double)firsts[col] + m, 1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps)); // an infinity or NaN in a sample: NaN, and
+        if (r0 == 0 && stats) {                                                                              // so is all of its result
+            stats[col] = out.x;
+            stats[a.B + col] = out.y;
         }
-    }
-    add_up<V>(s1, s2, sh.cl_log2, lds);
-    if ((int)threadIdx.x < 1 << sh.cl_log2 && col < sh.B)
+        return out;
+    });
+    if (!c.any()) return;
+    const PlainBlock in{x};
+    walk_rows<CL>(r0, r1, [&](int r, auto full, int left) {
+        PlainBlock::Raw t[NORM_ROWS];
+        float g[NORM_ROWS], b[NORM_ROWS];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            part[(size_t)blockIdx.y * sh.B + col + v] = make_double2(s1[v], s2[v]);
-            if (blockIdx.y == 0) firsts[col + v] = x[col + v];
-        }
-}
-
-// The sums of all ranges for a workgroup's columns, in all of its threads.
-template <int V>
-__device__ __forceinline__ void total(const double2 *__restrict__ part, int ranges, int col, const Shape &sh, double (&a)[V], double (&b)[V], double2 (*lds)[V])
-{
-#pragma unroll
-    for (int v = 0; v < V; ++v) a[v] = b[v] = 0.0;
-    if (col < sh.B)
-        for (int k = (int)(threadIdx.x >> sh.cl_log2); k < ranges; k += NORM_THREADS >> sh.cl_log2)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const double2 p = part[(size_t)k * sh.B + col + v];
-                a[v] += p.x;
-                b[v] += p.y;
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (full.value || u < left) {
+                const size_t row = (size_t)r + u * (NORM_THREADS / CL);
+                in.request(c, row, t[u]);
+                g[u] = gamma ? gamma[row] : 1.0f;
+                b[u] = beta ? beta[row] : 0.0f;
             }
-    add_up<V>(a, b, sh.cl_log2, lds);
-    const int c = threadIdx.x & ((1 << sh.cl_log2) - 1);
-    __syncthreads();
-    if ((int)threadIdx.x == c)
 #pragma unroll
-        for (int v = 0; v < V; ++v) lds[c][v] = make_double2(a[v], b[v]);
-    __syncthreads();
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (full.value || u < left) {
+                float o[4];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        a[v] = lds[c][v].x;
-        b[v] = lds[c][v].y;
-    }
+                for (int v = 0; v < 4; ++v) o[v] = (float)fma(((double)t[u].v[v] - mean[v]) * rstd[v], (double)g[u], (double)b[u]);
+                store_row(c, y + ((size_t)r + u * (NORM_THREADS / CL)) * a.B + c.base, o);
+            }
+    });
 }
 
-template <int V> __device__ __forceinline__ void store(float *p, const float (&v)[V])
+// Eight sums over the CL lanes of a row: afterwards p[0 ..] of a lane are those from `first` on, as many as the return value, and `keep`
+// says whether it is the lane that has them to store.
+template <int CL> __device__ __forceinline__ int add_columns(double (&p)[8], int lane, int &first, bool &keep)
 {
-    if constexpr (V == 4) *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    else *p = v[0];
-}
-
-template <int V>
-__global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, const float *__restrict__ gamma, const float *__restrict__ beta, Shape sh,
-                                                             double eps, const double2 *__restrict__ part, float *y, double *__restrict__ stats, int ranges,
-                                                             const float *__restrict__ firsts)
-{
-    __shared__ double2 lds[NORM_THREADS][V];
-    const int col = ((int)(blockIdx.x << sh.cl_log2) + (int)(threadIdx.x & ((1 << sh.cl_log2) - 1))) * V;
-    double mean[V], rstd[V];
-    total<V>(part, ranges, col, sh, mean, rstd, lds);
-    if (col >= sh.B) return;
-    const double inv = 1.0 / (double)sh.n;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const double m = mean[v] * inv, var = rstd[v] * inv - m * m;
-        mean[v] = (double)firsts[col + v] + m;
-        rstd[v] = 1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps); // an infinity or NaN in a sample: NaN, and so is all of its result
-    }
-    if (blockIdx.y == 0 && stats && (int)threadIdx.x < 1 << sh.cl_log2)
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            stats[col + v] = mean[v];
-            stats[sh.B + col + v] = rstd[v];
-        }
-    const int r0 = (int)blockIdx.y * sh.rows, r1 = min(sh.n, r0 + sh.rows);
-    for (int r = r0 + (int)(threadIdx.x >> sh.cl_log2); r < r1; r += NORM_THREADS >> sh.cl_log2) {
-        const double g = gamma ? (double)gamma[r] : 1.0, b = beta ? (double)beta[r] : 0.0;
-        float t[V];
-        PlainBlock{x}.load<V>((size_t)r * sh.B + col, t);
-#pragma unroll
-        for (int v = 0; v < V; ++v) t[v] = (float)fma(((double)t[v] - mean[v]) * rstd[v], g, b);
-        store<V>(y + (size_t)r * sh.B + col, t);
+    keep = true;
+    if constexpr (CL == 1) {
+        first = 0;
+        return 8;
+    } else if constexpr (CL == 4) {
+        halve<8, 1>(p, lane);
+        halve<4, 0>(p, lane);
+        first = 2 * (2 * (lane >> 1 & 1) + (lane & 1));
+        return 2;
+    } else {
+        constexpr int BIT = CL == 64 ? 5 : CL == 32 ? 4 : CL == 16 ? 3 : 2;
+        halve<8, BIT>(p, lane);
+        halve<4, BIT - 1>(p, lane);
+        halve<2, BIT - 2>(p, lane);
+        if constexpr (CL >= 64) p[0] += lane_exchange<2>(p[0]);
+        if constexpr (CL >= 32) p[0] += lane_exchange<1>(p[0]);
+        if constexpr (CL >= 16) p[0] += lane_exchange<0>(p[0]);
+        first = 4 * (lane >> BIT & 1) + 2 * (lane >> (BIT - 1) & 1) + (lane >> (BIT - 2) & 1);
+        keep = (lane & (CL / 8 - 1)) == 0;
+        return 1;
     }
 }
 
-// The backward pass's sums: over a range of rows p = sum g dY and q = sum g dY h for every sample, h = (x - mean) rstd, and over the
-// samples dg = sum dY h and db = sum dY for every row of the range.
-#define GRAD_ROWS 512 // rows of a range at most
-template <int V, class Block>
+// Where the sums along the rows go: dgamma and dbeta, or (more than one tile across) row_part [tile][n][2].
+struct RowSums {
+    double *part;
+    float *dgamma, *dbeta;
+};
+
+// part [range][B]: sums of g dY and of g dY h over the rows of a range, h = (x - mean) rstd; and the sums of dY h and dY over the
+// tile's columns.
+template <int CL, bool SMALL, class Block>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__restrict__ dy, const Block x, const double *__restrict__ stats,
-                                                                 const float *__restrict__ gamma, Shape sh, double2 *__restrict__ part,
-                                                                 float *__restrict__ dgamma, float *__restrict__ dbeta)
+                                                                 const float *__restrict__ gamma, const NormArgs a, double2 *__restrict__ part, const RowSums rs)
 {
-    __shared__ double2 lds[NORM_THREADS][V], row_sum[GRAD_ROWS];
-    const int cl = 1 << sh.cl_log2, c = threadIdx.x & (cl - 1);
-    const int r0 = (int)blockIdx.x * sh.rows, r1 = min(sh.n, r0 + sh.rows);
-    for (int r = threadIdx.x; r < GRAD_ROWS; r += NORM_THREADS) row_sum[r] = make_double2(0.0, 0.0);
-    __syncthreads();
-    for (int col0 = 0; col0 < sh.B; col0 += cl * V) {
-        const int col = col0 + c * V;
-        const bool live = col < sh.B;
-        double p[V] = {}, q[V] = {}, mean[V] = {}, rstd[V] = {};
-        if (live)
+    static_assert(NORM_ROWS == 4, "eight sums at a time");
+    const int range = (int)blockIdx.x / a.tiles, lane = threadIdx.x & 63;
+    const int tile = a.tile0 + (int)blockIdx.x - range * a.tiles;
+    const Columns<CL, SMALL> c(tile, a.B);
+    const int r0 = range * a.rows, r1 = min(a.n, r0 + a.rows);
+    const PlainBlock up{dy};
+    double p[4] = {}, q[4] = {}, mean[4] = {}, rstd[4] = {};
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                mean[v] = stats[col + v];
-                rstd[v] = stats[sh.B + col + v];
+    for (int v = 0; v < 4; ++v)
+        if (c.any() && c.own(v)) {
+            mean[v] = stats[c.base + v];
+            rstd[v] = stats[a.B + c.base + v];
+        }
+    walk_rows<CL>(r0, r1, [&](int r, auto full, int left) {
+        PlainBlock::Raw d[NORM_ROWS];
+        typename Block::Raw t[NORM_ROWS];
+        float g[NORM_ROWS];
+#pragma unroll
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if ((full.value || u < left) && c.any()) {
+                const size_t row = (size_t)r + u * (NORM_THREADS / CL);
+                up.request(c, row, d[u]);
+                x.request(c, row, t[u]);
+                g[u] = gamma ? gamma[row] : 1.0f;
             }
-        for (int r = r0 + (int)(threadIdx.x >> sh.cl_log2); r < r1; r += NORM_THREADS >> sh.cl_log2) {
-            const double g = gamma ? (double)gamma[r] : 1.0;
-            double dg = 0.0, db = 0.0;
-            if (live) {
-                float t[V], d[V];
-                const size_t e = (size_t)r * sh.B + col;
-                x.template load<V>(e, t);
-                PlainBlock{dy}.load<V>(e, d);
+        double sum[8] = {};
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    const double h = ((double)t[v] - mean[v]) * rstd[v], gd = g * (double)d[v];
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if ((full.value || u < left) && c.any()) {
+                float xv[4];
+                x.values(t[u], xv);
+                if (c.ragged())
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+                        if (!c.own(v)) d[u].v[v] = xv[v] = 0.0f;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const double h = ((double)xv[v] - mean[v]) * rstd[v], dv = (double)d[u].v[v], gd = (double)g[u] * dv;
                     p[v] += gd;
                     q[v] = fma(gd, h, q[v]);
-                    dg = fma((double)d[v], h, dg);
-                    db += (double)d[v];
+                    sum[2 * u] = fma(dv, h, sum[2 * u]);
+                    sum[2 * u + 1] += dv;
                 }
             }
-            for (int m = 1; m < cl; m *= 2) {
-                dg += __shfl_xor(dg, m);
-                db += __shfl_xor(db, m);
-            }
-            if (c == 0) { // always the same thread for a row
-                row_sum[r - r0].x += dg;
-                row_sum[r - r0].y += db;
-            }
-        }
-        add_up<V>(p, q, sh.cl_log2, lds);
-        if ((int)threadIdx.x < cl && live)
+        int first;
+        bool keep;
+        const int n_sums = add_columns<CL>(sum, lane, first, keep);
+        if (keep)
 #pragma unroll
-            for (int v = 0; v < V; ++v) part[(size_t)blockIdx.x * sh.B + col + v] = make_double2(p[v], q[v]);
-    }
-    __syncthreads();
-    for (int r = r0 + (int)threadIdx.x; r < r1; r += NORM_THREADS) {
-        if (dgamma) dgamma[r] = (float)row_sum[r - r0].x;
-        if (dbeta) dbeta[r] = (float)row_sum[r - r0].y;
-    }
+            for (int j = 0; j < n_sums; ++j) {
+                const int u = (first + j) >> 1, w = (first + j) & 1;
+                const size_t row = (size_t)r + u * (NORM_THREADS / CL);
+                if (full.value || u < left) {
+                    if (rs.part) rs.part[2 * ((size_t)tile * a.n + row) + w] = sum[j];
+                    else if (w == 0 && rs.dgamma) rs.dgamma[row] = (float)sum[j];
+                    else if (w == 1 && rs.dbeta) rs.dbeta[row] = (float)sum[j];
+                }
+            }
+    });
+    store_column_sums<CL>(c, p, q, part + (size_t)range * a.B);
 }
 
-template <int V, class Block>
+// rs.part: not NULL in the last launch over the tiles of a block with more than one across.
+template <int CL, bool SMALL, class Block>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_apply(const float *dy, const Block x, const double *__restrict__ stats, const float *__restrict__ gamma,
-                                                                  Shape sh, const double2 *__restrict__ part, int ranges, float *dx)
+                                                                  const NormArgs a, const double2 *__restrict__ part, float *dx, const RowSums rs, int all_tiles)
 {
-    __shared__ double2 lds[NORM_THREADS][V];
-    const int col = ((int)(blockIdx.x << sh.cl_log2) + (int)(threadIdx.x & ((1 << sh.cl_log2) - 1))) * V;
-    double p[V], q[V], mean[V], rstd[V];
-    total<V>(part, ranges, col, sh, p, q, lds);
-    if (col >= sh.B) return;
-    const double inv = 1.0 / (double)sh.n;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        p[v] *= inv;
-        q[v] *= inv;
-        mean[v] = stats[col + v];
-        rstd[v] = stats[sh.B + col + v];
-    }
-    const int r0 = (int)blockIdx.y * sh.rows, r1 = min(sh.n, r0 + sh.rows);
-    for (int r = r0 + (int)(threadIdx.x >> sh.cl_log2); r < r1; r += NORM_THREADS >> sh.cl_log2) {
-        const double g = gamma ? (double)gamma[r] : 1.0;
-        float t[V], d[V];
-        const size_t e = (size_t)r * sh.B + col;
-        x.template load<V>(e, t);
-        PlainBlock{dy}.load<V>(e, d);
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const double h = ((double)t[v] - mean[v]) * rstd[v];
-            t[v] = (float)(rstd[v] * (fma(g, (double)d[v], -p[v]) - h * q[v]));
+    int tile, r0, r1;
+    second_tile(a, tile, r0, r1);
+    if (rs.part) { // the rows' sums: every tile across adds up a share of the range's
+        const int share = (r1 - r0 + a.tiles - 1) / a.tiles, e1 = 2 * min(r1, r0 + (tile - a.tile0 + 1) * share);
+        for (int e = 2 * (r0 + (tile - a.tile0) * share) + (int)threadIdx.x; e < e1; e += NORM_THREADS) {
+            double s = 0.0;
+            for (int k = 0; k < all_tiles; ++k) s += rs.part[2 * (size_t)k * a.n + e];
+            float *out = e & 1 ? rs.dbeta : rs.dgamma;
+            if (out) out[e >> 1] = (float)s;
         }
-        store<V>(dx + e, t);
     }
+    if (!dx) return;
+    const Columns<CL, SMALL> c(tile, a.B);
+    double p[4], q[4], mean[4] = {}, rstd[4] = {};
+    const double inv = 1.0 / (double)a.n;
+    load_column_sums<CL>(c, part, a.ranges, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
+    if (!c.any()) return;
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+        if (c.own(v)) {
+            mean[v] = stats[c.base + v];
+            rstd[v] = stats[a.B + c.base + v];
+        }
+    const PlainBlock up{dy};
+    walk_rows<CL>(r0, r1, [&](int r, auto full, int left) {
+        PlainBlock::Raw d[NORM_ROWS];
+        typename Block::Raw t[NORM_ROWS];
+        float g[NORM_ROWS];
+#pragma unroll
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (full.value || u < left) {
+                const size_t row = (size_t)r + u * (NORM_THREADS / CL);
+                up.request(c, row, d[u]);
+                x.request(c, row, t[u]);
+                g[u] = gamma ? gamma[row] : 1.0f;
+            }
+#pragma unroll
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (full.value || u < left) {
+                float xv[4], o[4];
+                x.values(t[u], xv);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const double h = ((double)xv[v] - mean[v]) * rstd[v];
+                    o[v] = (float)(rstd[v] * fma(-h, q[v], fma((double)g[u], (double)d[u].v[v], -p[v])));
+                }
+                store_row(c, dx + ((size_t)r + u * (NORM_THREADS / CL)) * a.B + c.base, o);
+            }
+    });
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
-// Ranges of rows: enough workgroups to fill the chip, and not so many that their sums are a load to add up.
-static int forward_ranges(int n, int B) { return std::max(1, std::min(1024 / ((B - 1) / 256 + 1), (n - 1) / 32 + 1)); }
-static int backward_ranges(int n) { return std::max(std::min(1024, (n - 1) / 16 + 1), (n - 1) / GRAD_ROWS + 1); }
-static int range_rows(int n, int ranges) { return (n - 1) / ranges + 1; }
+static int across(int B) { return B < 4 ? 1 : B <= 16 ? 4 : B <= 32 ? 8 : B <= 64 ? 16 : B <= 128 ? 32 : 64; } // lanes, CL
+static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-static Shape shape_for(int n, int B, int V, int ranges)
+// Tiles: enough workgroups to fill the chip, but not so many ranges that their sums are a load to add up.
+struct NormPlan {
+    NormArgs a;
+    size_t row_part, firsts, total; // bytes into the workspace
+};
+static NormPlan plan_norm(int n, int B)
 {
-    Shape sh;
-    sh.n = n; sh.B = B; sh.cl_log2 = 0; sh.rows = range_rows(n, ranges);
-    while (sh.cl_log2 < 6 && (V << sh.cl_log2) < B) ++sh.cl_log2;
-    return sh;
+    NormPlan p;
+    const int cl = across(B), unit = NORM_ROWS * NORM_THREADS / cl;
+    NormArgs &a = p.a;
+    a.n = n; a.B = B; a.tile0 = 0;
+    a.tiles = ceil_div(B, 4 * cl);
+    const int most = std::max(1, std::min(128, 512 / a.tiles));
+    a.rows = std::max(unit, ceil_div(ceil_div(n, most), unit) * unit);
+    a.ranges = ceil_div(n, a.rows);
+    a.splits = 1;
+    while (a.splits < 8 && (int64_t)a.ranges * a.tiles * a.splits < 256 && a.rows / (2 * a.splits) >= unit) a.splits *= 2;
+    p.row_part = 16 * (size_t)a.ranges * (size_t)B;
+    p.firsts = p.row_part + (a.tiles > 1 ? 16 * (size_t)a.tiles * (size_t)n : 0);
+    p.total = (p.firsts + 4 * (size_t)B + 255) & ~(size_t)255;
+    return p;
 }
-static unsigned tiles(const Shape &sh, int V) { return (unsigned)((sh.B - 1) / (V << sh.cl_log2) + 1); }
 
 static int check_norm(int32_t n, int32_t B)
 {
@@ -280,69 +477,84 @@ static int check_norm(int32_t n, int32_t B)
         return sdnn_fail(SDNN_EINVAL, "a block of %d x %d values: n and B from 1 to 2^30 and less than 2^40 values are wanted", n, B);
     return SDNN_OK;
 }
-static size_t workspace(int n, int B)
-{
-    return (16 * (size_t)std::max(forward_ranges(n, B), backward_ranges(n)) * (size_t)B + 4 * (size_t)B + 255) & ~(size_t)255;
-}
 static int check_work(const void *d_work, size_t work_bytes, int32_t n, int32_t B)
 {
     const int rc = check_norm(n, B);
     if (rc) return rc;
     if (!d_work) return sdnn_fail(SDNN_EINVAL, "d_work is NULL");
     if ((uintptr_t)d_work & 15) return sdnn_fail(SDNN_EINVAL, "d_work must be 16-byte aligned");
-    if (work_bytes < workspace(n, B)) return sdnn_fail(SDNN_ENOMEM, "workspace of %zu bytes, %zu needed", work_bytes, workspace(n, B));
+    const size_t need = plan_norm(n, B).total;
+    if (work_bytes < need) return sdnn_fail(SDNN_ENOMEM, "workspace of %zu bytes, %zu needed", work_bytes, need);
     return SDNN_OK;
 }
-static bool wide(int B, const void *a, const void *b) { return B % 4 == 0 && (((uintptr_t)a | (uintptr_t)b) & 15) == 0; }
 
 extern "C" int sdnn_layernorm_workspace_bytes(int32_t n, int32_t B, size_t *bytes)
 {
     if (!bytes) return sdnn_fail(SDNN_EINVAL, "bytes is NULL");
     const int rc = check_norm(n, B);
     if (rc) return rc;
-    *bytes = workspace(n, B);
+    *bytes = plan_norm(n, B).total;
     return SDNN_OK;
 }
 
-template <int V>
-static int forward(const float *x, const float *gamma, const float *beta, int n, int B, double eps, float *y, double *stats, void *work, hipStream_t stream)
+template <int CL, bool SMALL>
+static int forward(const float *x, const float *gamma, const float *beta, double eps, float *y, double *stats, void *work, const NormPlan &pl, hipStream_t stream)
 {
-    const int ranges = forward_ranges(n, B);
-    const Shape sh = shape_for(n, B, V, ranges);
     double2 *part = (double2 *)work;
-    float *firsts = (float *)(part + (size_t)ranges * B);
-    const dim3 grid(tiles(sh, V), (unsigned)ranges);
-    hipLaunchKernelGGL(k_norm_sums<V>, grid, dim3(NORM_THREADS), 0, stream, x, sh, part, firsts);
-    hipLaunchKernelGGL(k_norm_apply<V>, grid, dim3(NORM_THREADS), 0, stream, x, gamma, beta, sh, eps, part, y, stats, ranges, firsts);
+    float *firsts = (float *)((char *)work + pl.firsts);
+    const NormArgs &a = pl.a;
+    hipLaunchKernelGGL((k_norm_sums<CL, SMALL>), dim3((unsigned)(a.tiles * a.ranges)), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
+    hipLaunchKernelGGL((k_norm_apply<CL, SMALL>), dim3((unsigned)(a.tiles * a.ranges * a.splits)), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts,
+                       y, stats);
     return sdnn_launched();
 }
 
 extern "C" int sdnn_layernorm(const float *d_X, const float *d_gamma, const float *d_beta, int32_t n, int32_t B, double eps, float *d_Y,
-                              double *d_stats, void *d_work, size_t work_bytes, void *stream)
+                              double *d_stats, void *d_work, size_t work_bytes, void *stream_)
 {
     const int rc = check_work(d_work, work_bytes, n, B);
     if (rc) return rc;
     if (!d_X || !d_Y) return sdnn_fail(SDNN_EINVAL, "d_X or d_Y is NULL");
     if (!(eps > 0.0) || !(eps <= 1e30)) return sdnn_fail(SDNN_EINVAL, "eps must be > 0");
-    return wide(B, d_X, d_Y) ? forward<4>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, d_work, (hipStream_t)stream)
-                             : forward<1>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, d_work, (hipStream_t)stream);
+    const NormPlan pl = plan_norm(n, B);
+    hipStream_t stream = (hipStream_t)stream_;
+    switch (across(B)) {
+    case 1: return forward<1, true>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 4: return forward<4, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 8: return forward<8, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 16: return forward<16, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 32: return forward<32, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    default: return forward<64, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    }
 }
 
-template <int V, class Block>
-static int backward(const float *dy, const Block &x, const double *stats, const float *gamma, int n, int B, float *dx, float *dgamma, float *dbeta, void *work,
-                    hipStream_t stream)
+template <int CL, bool SMALL, class Block>
+static int backward(const float *dy, const Block &x, const double *stats, const float *gamma, float *dx, RowSums rs, void *work, const NormPlan &pl, hipStream_t stream)
 {
-    const int ranges = backward_ranges(n);
-    Shape sh = shape_for(n, B, V, ranges);
     double2 *part = (double2 *)work;
-    hipLaunchKernelGGL((k_norm_grad_sums<V, Block>), dim3((unsigned)range_rows(n, sh.rows)), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, sh, part, dgamma, dbeta);
-    const int used = range_rows(n, sh.rows); // ranges that have rows
-    if (dx) {
-        const int f = forward_ranges(n, B);
-        sh.rows = range_rows(n, f);
-        hipLaunchKernelGGL((k_norm_grad_apply<V, Block>), dim3(tiles(sh, V), (unsigned)f), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, sh, part, used, dx);
-    }
+    const NormArgs &a = pl.a;
+    rs.part = a.tiles > 1 ? (double *)((char *)work + pl.row_part) : nullptr;
+    hipLaunchKernelGGL((k_norm_grad_sums<CL, SMALL, Block>), dim3((unsigned)(a.tiles * a.ranges)), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, rs);
+    if (dx || rs.part)
+        hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, Block>), dim3((unsigned)(a.tiles * a.ranges * a.splits)), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma,
+                           a, part, dx, rs, a.tiles);
     return sdnn_launched();
+}
+template <class Block>
+static int backward_any(const float *dy, const Block &x, const double *stats, const float *gamma, int n, int B, float *dx, float *dgamma, float *dbeta, void *work,
+                        void *stream_)
+{
+    const NormPlan pl = plan_norm(n, B);
+    const RowSums rs{nullptr, dgamma, dbeta};
+    hipStream_t stream = (hipStream_t)stream_;
+    switch (across(B)) {
+    case 1: return backward<1, true>(dy, x, stats, gamma, dx, rs, work, pl, stream);
+    case 4: return backward<4, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
+    case 8: return backward<8, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
+    case 16: return backward<16, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
+    case 32: return backward<32, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
+    default: return backward<64, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
+    }
 }
 
 static int check_backward(const float *d_dY, const double *d_stats, const float *d_dX, const float *d_dgamma, const float *d_dbeta)
@@ -359,10 +571,7 @@ extern "C" int sdnn_layernorm_backward(const float *d_dY, const float *d_X, cons
     if (!rc) rc = check_backward(d_dY, d_stats, d_dX, d_dgamma, d_dbeta);
     if (rc) return rc;
     if (!d_X) return sdnn_fail(SDNN_EINVAL, "d_X is NULL");
-    const PlainBlock x{d_X};
-    return wide(B, d_X, d_dY) && wide(B, d_dX, nullptr)
-               ? backward<4>(d_dY, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, (hipStream_t)stream)
-               : backward<1>(d_dY, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, (hipStream_t)stream);
+    return backward_any(d_dY, PlainBlock{d_X}, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
 }
 
 extern "C" int sdnn_layernorm_backward_packed(const float *d_dY, const void *d_packed, size_t packed_bytes, float cap, const double *d_stats,
@@ -377,6 +586,5 @@ extern "C" int sdnn_layernorm_backward_packed(const float *d_dY, const void *d_p
     x.codes = (const uint8_t *)d_packed;
     x.scales = (const uint16_t *)(x.codes + PACK_GROUP * pack8_groups((int64_t)n * B));
     x.cap = cap; x.below = nextafterf(cap, 0.0f);
-    return wide(B, d_dX, d_dY) ? backward<4>(d_dY, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, (hipStream_t)stream)
-                               : backward<1>(d_dY, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, (hipStream_t)stream);
+    return backward_any(d_dY, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
 }
