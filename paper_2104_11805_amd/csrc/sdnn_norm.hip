@@ -132,7 +132,7 @@ __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__re
     const int tid = threadIdx.x, col = c.tile0 + (tid & (CT - 1));
     double2 s = make_double2(0.0, 0.0);
     if (col < c.B)
-#pragma unroll 4
+#pragma unroll 8
         for (int k = tid / CT; k < ranges; k += K) {
             const double2 t = part[(size_t)k * c.B + col];
             s.x += t.x;
@@ -157,77 +157,64 @@ __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__re
     }
 }
 
-// The rows that a thread walks: r0 + its place, in steps of NORM_THREADS / CL, NORM_ROWS of them at a time; body(row of each, how many of
-// them there are: NORM_ROWS but at a range's end).
-template <int CL, class F> __device__ __forceinline__ void walk_rows(int r0, int r1, F body)
-{
-    constexpr int STEP = NORM_THREADS / CL;
-    for (int r = r0 + (int)threadIdx.x / CL; r < r1; r += NORM_ROWS * STEP) {
-        const int left = (r1 - r + STEP - 1) / STEP;
-        if (left >= NORM_ROWS) body(r, std::integral_constant<bool, true>(), NORM_ROWS);
-        else body(r, std::integral_constant<bool, false>(), left);
-    }
-}
+// The rows that a thread walks: its first one, and NORM_ROWS of them at a time, row_of<CL>(r, u), of those below r1.
+template <int CL> __device__ __forceinline__ int first_row(int r0) { return r0 + (int)threadIdx.x / CL; }
+template <int CL> __device__ __forceinline__ int row_of(int r, int u) { return r + u * (NORM_THREADS / CL); }
+template <int CL> __device__ __forceinline__ int next_rows(int r) { return row_of<CL>(r, NORM_ROWS); }
 
 struct NormArgs {
-    int32_t n, B, rows; // rows of a range
-    int32_t tiles, tile0, splits, ranges; // tiles of columns in this launch, the first of them; second launches: parts of a range, ranges
+    int32_t n, B, rows;            // rows of a range
+    int32_t tiles, ranges, splits; // tiles across; ranges; second launches: parts of a range
 };
+// Which part a workgroup takes.  Workgroup ids go round the XCDs: an XCD takes whole rows of the block (a tile's columns of all rows lie
+// in the same few of an L2's channels), and in the second launch those that it had in the first.  Few ranges: any.
+__device__ __forceinline__ bool find_tile(const NormArgs &a, int splits, int &tile, int &range, int &r0, int &r1)
+{
+    const unsigned across = (unsigned)a.tiles * (unsigned)splits, id = a.ranges < 8 ? blockIdx.x : blockIdx.x >> 3;
+    range = (int)(id / across);
+    if (a.ranges >= 8) range = 8 * range + (int)(blockIdx.x & 7);
+    if (range >= a.ranges) return false;
+    const unsigned at = id % across, split = at / (unsigned)a.tiles;
+    tile = (int)(at % (unsigned)a.tiles);
+    const int rows = (a.rows + splits - 1) / splits;
+    r0 = min(a.n, range * a.rows + (int)split * rows);
+    r1 = min(min(a.n, (range + 1) * a.rows), r0 + rows);
+    return true;
+}
 
 // part [range][B]: sums of x - x0 and of its square, x0 the sample's first value: nothing cancels where the mean is large.
 // firsts [B]: x0, which the second launch may write its results over.
 template <int CL, bool SMALL>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restrict__ x, const NormArgs a, double2 *__restrict__ part, float *__restrict__ firsts)
 {
-    const int range = (int)blockIdx.x / a.tiles;
-    const Columns<CL, SMALL> c(a.tile0 + (int)blockIdx.x - range * a.tiles, a.B);
-    const int r0 = range * a.rows, r1 = min(a.n, r0 + a.rows);
+    int tile, range, r0, r1;
+    if (!find_tile(a, 1, tile, range, r0, r1)) return;
+    const Columns<CL, SMALL> c(tile, a.B);
     const PlainBlock in{x};
     double s1[4] = {}, s2[4] = {};
     if (c.any()) {
-        PlainBlock::Raw first;
+        PlainBlock::Raw first, t[NORM_ROWS];
         in.request(c, 0, first);
         if (range == 0 && (int)threadIdx.x < CL)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
                 if (c.own(v)) firsts[c.base + v] = first.v[v];
-        walk_rows<CL>(r0, r1, [&](int r, auto full, int left) {
-            PlainBlock::Raw t[NORM_ROWS];
+        for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r)) {
 #pragma unroll
             for (int u = 0; u < NORM_ROWS; ++u)
-                if (full.value || u < left) in.request(c, (size_t)r + u * (NORM_THREADS / CL), t[u]);
+                if (row_of<CL>(r, u) < r1) in.request(c, row_of<CL>(r, u), t[u]);
 #pragma unroll
             for (int u = 0; u < NORM_ROWS; ++u)
-                if (full.value || u < left)
+                if (row_of<CL>(r, u) < r1)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         const double d = (double)t[u].v[v] - (double)first.v[v];
                         s1[v] += d;
                         s2[v] = fma(d, d, s2[v]);
                     }
-        });
+        }
     }
     store_column_sums<CL>(c, s1, s2, part + (size_t)range * a.B);
-}
-
-// Which tile a workgroup of a second launch takes: the ranges of the first launch in `splits` parts, each on the XCD that has read it.
-__device__ __forceinline__ void second_tile(const NormArgs &a, int &tile, int &r0, int &r1)
-{
-    const unsigned all = (unsigned)a.tiles * (unsigned)a.ranges, whole = all & ~7u;
-    unsigned id, split;
-    if (blockIdx.x < whole * (unsigned)a.splits) {
-        const unsigned j = blockIdx.x >> 3;
-        id = 8 * (j / (unsigned)a.splits) + (blockIdx.x & 7);
-        split = j % (unsigned)a.splits;
-    } else {
-        const unsigned j = blockIdx.x - whole * (unsigned)a.splits;
-        id = whole + j / (unsigned)a.splits;
-        split = j % (unsigned)a.splits;
-    }
-    const int range = (int)(id / (unsigned)a.tiles), rows = (a.rows + a.splits - 1) / a.splits;
-    tile = a.tile0 + (int)(id % (unsigned)a.tiles);
-    r0 = min(a.n, range * a.rows + (int)split * rows);
-    r1 = min(min(a.n, (range + 1) * a.rows), r0 + rows);
 }
 
 template <class C> __device__ __forceinline__ void store_row(const C &c, float *p, const float (&o)[4])
@@ -249,9 +236,25 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
                                                              double eps, const double2 *__restrict__ part, const float *__restrict__ firsts, float *y,
                                                              double *__restrict__ stats)
 {
-    int tile, r0, r1;
-    second_tile(a, tile, r0, r1);
+    int tile, range, r0, r1;
+    if (!find_tile(a, a.splits, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
+    const PlainBlock in{x};
+    struct Rows {
+        PlainBlock::Raw t[NORM_ROWS];
+        float g[NORM_ROWS], b[NORM_ROWS];
+    } now, next;
+    auto request = [&](int r, Rows &w) {
+#pragma unroll
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (row_of<CL>(r, u) < r1 && c.any()) {
+                in.request(c, row_of<CL>(r, u), w.t[u]);
+                w.g[u] = gamma ? gamma[row_of<CL>(r, u)] : 1.0f;
+                w.b[u] = beta ? beta[row_of<CL>(r, u)] : 0.0f;
+            }
+    };
+    int r = first_row<CL>(r0);
+    request(r, now); // on their way while the sums are added up
     double mean[4], rstd[4];
     const double inv = 1.0 / (double)a.n;
     load_column_sums<CL>(c, part, a.ranges, mean, rstd, [&](int col, double2 s) {
@@ -264,27 +267,17 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
         return out;
     });
     if (!c.any()) return;
-    const PlainBlock in{x};
-    walk_rows<CL>(r0, r1, [&](int r, auto full, int left) {
-        PlainBlock::Raw t[NORM_ROWS];
-        float g[NORM_ROWS], b[NORM_ROWS];
+    for (; r < r1; r = next_rows<CL>(r), now = next) {
+        request(next_rows<CL>(r), next);
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (full.value || u < left) {
-                const size_t row = (size_t)r + u * (NORM_THREADS / CL);
-                in.request(c, row, t[u]);
-                g[u] = gamma ? gamma[row] : 1.0f;
-                b[u] = beta ? beta[row] : 0.0f;
-            }
-#pragma unroll
-        for (int u = 0; u < NORM_ROWS; ++u)
-            if (full.value || u < left) {
+            if (row_of<CL>(r, u) < r1) {
                 float o[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) o[v] = (float)fma(((double)t[u].v[v] - mean[v]) * rstd[v], (double)g[u], (double)b[u]);
-                store_row(c, y + ((size_t)r + u * (NORM_THREADS / CL)) * a.B + c.base, o);
+                for (int v = 0; v < 4; ++v) o[v] = (float)fma(((double)now.t[u].v[v] - mean[v]) * rstd[v], (double)now.g[u], (double)now.b[u]);
+                store_row(c, y + (size_t)row_of<CL>(r, u) * a.B + c.base, o);
             }
-    });
+    }
 }
 
 // Eight sums over the CL lanes of a row: afterwards p[0 ..] of a lane are those from `first` on, as many as the return value, and `keep`
@@ -327,10 +320,10 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
                                                                  const float *__restrict__ gamma, const NormArgs a, double2 *__restrict__ part, const RowSums rs)
 {
     static_assert(NORM_ROWS == 4, "eight sums at a time");
-    const int range = (int)blockIdx.x / a.tiles, lane = threadIdx.x & 63;
-    const int tile = a.tile0 + (int)blockIdx.x - range * a.tiles;
+    const int lane = threadIdx.x & 63;
+    int tile, range, r0, r1;
+    if (!find_tile(a, 1, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
-    const int r0 = range * a.rows, r1 = min(a.n, r0 + a.rows);
     const PlainBlock up{dy};
     double p[4] = {}, q[4] = {}, mean[4] = {}, rstd[4] = {};
 #pragma unroll
@@ -339,14 +332,14 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
             mean[v] = stats[c.base + v];
             rstd[v] = stats[a.B + c.base + v];
         }
-    walk_rows<CL>(r0, r1, [&](int r, auto full, int left) {
+    for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r)) {
         PlainBlock::Raw d[NORM_ROWS];
         typename Block::Raw t[NORM_ROWS];
         float g[NORM_ROWS];
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if ((full.value || u < left) && c.any()) {
-                const size_t row = (size_t)r + u * (NORM_THREADS / CL);
+            if (row_of<CL>(r, u) < r1 && c.any()) {
+                const size_t row = (size_t)row_of<CL>(r, u);
                 up.request(c, row, d[u]);
                 x.request(c, row, t[u]);
                 g[u] = gamma ? gamma[row] : 1.0f;
@@ -354,7 +347,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
         double sum[8] = {};
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if ((full.value || u < left) && c.any()) {
+            if (row_of<CL>(r, u) < r1 && c.any()) {
                 float xv[4];
                 x.values(t[u], xv);
                 if (c.ragged())
@@ -377,35 +370,53 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
 #pragma unroll
             for (int j = 0; j < n_sums; ++j) {
                 const int u = (first + j) >> 1, w = (first + j) & 1;
-                const size_t row = (size_t)r + u * (NORM_THREADS / CL);
-                if (full.value || u < left) {
+                const size_t row = (size_t)row_of<CL>(r, u);
+                if (row < (size_t)r1) {
                     if (rs.part) rs.part[2 * ((size_t)tile * a.n + row) + w] = sum[j];
                     else if (w == 0 && rs.dgamma) rs.dgamma[row] = (float)sum[j];
                     else if (w == 1 && rs.dbeta) rs.dbeta[row] = (float)sum[j];
                 }
             }
-    });
+    }
     store_column_sums<CL>(c, p, q, part + (size_t)range * a.B);
 }
 
 // rs.part: not NULL in the last launch over the tiles of a block with more than one across.
 template <int CL, bool SMALL, class Block>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_apply(const float *dy, const Block x, const double *__restrict__ stats, const float *__restrict__ gamma,
-                                                                  const NormArgs a, const double2 *__restrict__ part, float *dx, const RowSums rs, int all_tiles)
+                                                                  const NormArgs a, const double2 *__restrict__ part, float *dx, const RowSums rs)
 {
-    int tile, r0, r1;
-    second_tile(a, tile, r0, r1);
+    int tile, range, r0, r1;
+    if (!find_tile(a, a.splits, tile, range, r0, r1)) return;
     if (rs.part) { // the rows' sums: every tile across adds up a share of the range's
-        const int share = (r1 - r0 + a.tiles - 1) / a.tiles, e1 = 2 * min(r1, r0 + (tile - a.tile0 + 1) * share);
-        for (int e = 2 * (r0 + (tile - a.tile0) * share) + (int)threadIdx.x; e < e1; e += NORM_THREADS) {
+        const int share = (r1 - r0 + a.tiles - 1) / a.tiles, e1 = 2 * min(r1, r0 + (tile + 1) * share);
+        for (int e = 2 * (r0 + tile * share) + (int)threadIdx.x; e < e1; e += NORM_THREADS) {
             double s = 0.0;
-            for (int k = 0; k < all_tiles; ++k) s += rs.part[2 * (size_t)k * a.n + e];
+#pragma unroll 4
+            for (int k = 0; k < a.tiles; ++k) s += rs.part[2 * (size_t)k * a.n + e];
             float *out = e & 1 ? rs.dbeta : rs.dgamma;
             if (out) out[e >> 1] = (float)s;
         }
     }
     if (!dx) return;
     const Columns<CL, SMALL> c(tile, a.B);
+    const PlainBlock up{dy};
+    struct Rows {
+        PlainBlock::Raw d[NORM_ROWS];
+        typename Block::Raw t[NORM_ROWS];
+        float g[NORM_ROWS];
+    } now, next;
+    auto request = [&](int r, Rows &w) {
+#pragma unroll
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (row_of<CL>(r, u) < r1 && c.any()) {
+                up.request(c, row_of<CL>(r, u), w.d[u]);
+                x.request(c, row_of<CL>(r, u), w.t[u]);
+                w.g[u] = gamma ? gamma[row_of<CL>(r, u)] : 1.0f;
+            }
+    };
+    int r = first_row<CL>(r0);
+    request(r, now); // on their way while the sums are added up
     double p[4], q[4], mean[4] = {}, rstd[4] = {};
     const double inv = 1.0 / (double)a.n;
     load_column_sums<CL>(c, part, a.ranges, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
@@ -416,32 +427,21 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_apply(const float *d
             mean[v] = stats[c.base + v];
             rstd[v] = stats[a.B + c.base + v];
         }
-    const PlainBlock up{dy};
-    walk_rows<CL>(r0, r1, [&](int r, auto full, int left) {
-        PlainBlock::Raw d[NORM_ROWS];
-        typename Block::Raw t[NORM_ROWS];
-        float g[NORM_ROWS];
+    for (; r < r1; r = next_rows<CL>(r), now = next) {
+        request(next_rows<CL>(r), next);
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (full.value || u < left) {
-                const size_t row = (size_t)r + u * (NORM_THREADS / CL);
-                up.request(c, row, d[u]);
-                x.request(c, row, t[u]);
-                g[u] = gamma ? gamma[row] : 1.0f;
-            }
-#pragma unroll
-        for (int u = 0; u < NORM_ROWS; ++u)
-            if (full.value || u < left) {
+            if (row_of<CL>(r, u) < r1) {
                 float xv[4], o[4];
-                x.values(t[u], xv);
+                x.values(now.t[u], xv);
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     const double h = ((double)xv[v] - mean[v]) * rstd[v];
-                    o[v] = (float)(rstd[v] * fma(-h, q[v], fma((double)g[u], (double)d[u].v[v], -p[v])));
+                    o[v] = (float)(rstd[v] * fma(-h, q[v], fma((double)now.g[u], (double)now.d[u].v[v], -p[v])));
                 }
-                store_row(c, dx + ((size_t)r + u * (NORM_THREADS / CL)) * a.B + c.base, o);
+                store_row(c, dx + (size_t)row_of<CL>(r, u) * a.B + c.base, o);
             }
-    });
+    }
 }
 
 // ---- host side ------------------------------------------------------------------------------------------------------------
@@ -451,25 +451,31 @@ static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 // Tiles: enough workgroups to fill the chip, but not so many ranges that their sums are a load to add up.
 struct NormPlan {
     NormArgs a;
+    int cl;
     size_t row_part, firsts, total; // bytes into the workspace
 };
 static NormPlan plan_norm(int n, int B)
 {
     NormPlan p;
-    const int cl = across(B), unit = NORM_ROWS * NORM_THREADS / cl;
     NormArgs &a = p.a;
-    a.n = n; a.B = B; a.tile0 = 0;
-    a.tiles = ceil_div(B, 4 * cl);
-    const int most = std::max(1, std::min(128, 512 / a.tiles));
-    a.rows = std::max(unit, ceil_div(ceil_div(n, most), unit) * unit);
-    a.ranges = ceil_div(n, a.rows);
+    a.n = n; a.B = B;
+    const int most = std::max(1, (int)std::sqrt(n / 4.0)); // the second launch reads 16 bytes per range and column, and 4 per row
+    int unit;
+    for (p.cl = across(B);; p.cl /= 2) { // narrower tiles where there would be few
+        unit = NORM_ROWS * NORM_THREADS / p.cl;
+        a.tiles = ceil_div(B, 4 * p.cl);
+        a.rows = std::max(unit, ceil_div(ceil_div(n, std::max(1, std::min(most, 1024 / a.tiles))), unit) * unit);
+        a.ranges = ceil_div(n, a.rows);
+        if (p.cl <= 16 || (int64_t)a.tiles * a.ranges >= 256) break;
+    }
     a.splits = 1;
-    while (a.splits < 8 && (int64_t)a.ranges * a.tiles * a.splits < 256 && a.rows / (2 * a.splits) >= unit) a.splits *= 2;
+    while (a.splits < 8 && (int64_t)a.ranges * a.tiles * a.splits < 512 && a.rows / (2 * a.splits) >= unit) a.splits *= 2;
     p.row_part = 16 * (size_t)a.ranges * (size_t)B;
     p.firsts = p.row_part + (a.tiles > 1 ? 16 * (size_t)a.tiles * (size_t)n : 0);
     p.total = (p.firsts + 4 * (size_t)B + 255) & ~(size_t)255;
     return p;
 }
+static dim3 norm_grid(const NormArgs &a, int splits) { return dim3((unsigned)(a.tiles * splits * (a.ranges < 8 ? a.ranges : (a.ranges + 7) & ~7))); }
 
 static int check_norm(int32_t n, int32_t B)
 {
@@ -503,8 +509,8 @@ static int forward(const float *x, const float *gamma, const float *beta, double
     double2 *part = (double2 *)work;
     float *firsts = (float *)((char *)work + pl.firsts);
     const NormArgs &a = pl.a;
-    hipLaunchKernelGGL((k_norm_sums<CL, SMALL>), dim3((unsigned)(a.tiles * a.ranges)), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
-    hipLaunchKernelGGL((k_norm_apply<CL, SMALL>), dim3((unsigned)(a.tiles * a.ranges * a.splits)), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts,
+    hipLaunchKernelGGL((k_norm_sums<CL, SMALL>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
+    hipLaunchKernelGGL((k_norm_apply<CL, SMALL>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts,
                        y, stats);
     return sdnn_launched();
 }
@@ -518,7 +524,7 @@ extern "C" int sdnn_layernorm(const float *d_X, const float *d_gamma, const floa
     if (!(eps > 0.0) || !(eps <= 1e30)) return sdnn_fail(SDNN_EINVAL, "eps must be > 0");
     const NormPlan pl = plan_norm(n, B);
     hipStream_t stream = (hipStream_t)stream_;
-    switch (across(B)) {
+    switch (pl.cl) {
     case 1: return forward<1, true>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
     case 4: return forward<4, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
     case 8: return forward<8, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
@@ -534,10 +540,10 @@ static int backward(const float *dy, const Block &x, const double *stats, const 
     double2 *part = (double2 *)work;
     const NormArgs &a = pl.a;
     rs.part = a.tiles > 1 ? (double *)((char *)work + pl.row_part) : nullptr;
-    hipLaunchKernelGGL((k_norm_grad_sums<CL, SMALL, Block>), dim3((unsigned)(a.tiles * a.ranges)), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, rs);
+    hipLaunchKernelGGL((k_norm_grad_sums<CL, SMALL, Block>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, rs);
     if (dx || rs.part)
-        hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, Block>), dim3((unsigned)(a.tiles * a.ranges * a.splits)), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma,
-                           a, part, dx, rs, a.tiles);
+        hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma,
+                           a, part, dx, rs);
     return sdnn_launched();
 }
 template <class Block>
@@ -547,7 +553,7 @@ static int backward_any(const float *dy, const Block &x, const double *stats, co
     const NormPlan pl = plan_norm(n, B);
     const RowSums rs{nullptr, dgamma, dbeta};
     hipStream_t stream = (hipStream_t)stream_;
-    switch (across(B)) {
+    switch (pl.cl) {
     case 1: return backward<1, true>(dy, x, stats, gamma, dx, rs, work, pl, stream);
     case 4: return backward<4, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
     case 8: return backward<8, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);

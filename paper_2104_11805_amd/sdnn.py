@@ -164,8 +164,9 @@ def sdnn_deal_rows_to_xcds(n_rows, row_ptr, order):
 
 def _stream_ptr(stream=None):
     import torch
-    s = torch.cuda.current_stream() if stream is None else stream
-    return C.c_void_p(s.cuda_stream)
+    if stream is None:  # the current one, without making an object of it (2.7 us)
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    return C.c_void_p(stream.cuda_stream)
 
 
 def _dp(t):
@@ -176,50 +177,43 @@ def _dp(t):
     return C.c_void_p(t.data_ptr())
 
 
-def _tensor(t, name, shape, dtype, device, least=False):
-    """Checks a device tensor of a call on blocks: its shape (least: at least that many elements), type, device and layout."""
+def _tensor(t, name, shape, dtype, index):
+    """A device tensor of a call on blocks, after checks of its shape, type, device and layout."""
     import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device != device:
-        raise SdnnError(SDNN_EINVAL, f"{name} must be a tensor on {device}")
-    if t.dtype != dtype:
-        raise SdnnError(SDNN_EINVAL, f"{name} must be {dtype}, not {t.dtype}")
-    if not t.is_contiguous():
-        raise SdnnError(SDNN_EINVAL, f"{name} must be contiguous")
-    if t.numel() < shape[0] if least else tuple(t.shape) != tuple(shape):
-        raise SdnnError(SDNN_EINVAL, f"{name} has shape {tuple(t.shape)}, {tuple(shape)} {'at least ' if least else ''}is wanted")
-    return t
+    if isinstance(t, torch.Tensor) and t.get_device() == index and t.dtype is dtype and t.shape == shape and t.is_contiguous() and index >= 0:
+        return t
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise SdnnError(SDNN_EINVAL, f"{name} must be a tensor on the GPU")
+    if t.get_device() != index:
+        raise SdnnError(SDNN_EINVAL, f"{name} is on GPU {t.get_device()}, not on {index}")
+    raise SdnnError(SDNN_EINVAL, f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
 
 
-class _On:
-    """The device of a call's tensors as the current one, and the stream of the call as the current one, for what the call
-    allocates and launches."""
-
-    def __init__(self, device, stream):
-        import torch
-        self.device = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-        self.stream = None if stream is None else torch.cuda.stream(stream)
-
-    def __enter__(self):
-        if self.device is not None:
-            self.device.__enter__()
-        if self.stream is not None:
-            self.stream.__enter__()
-        return _stream_ptr()
-
-    def __exit__(self, *exc):
-        if self.stream is not None:
-            self.stream.__exit__(*exc)
-        if self.device is not None:
-            self.device.__exit__(*exc)
+def _bytes(t, name, index):
+    """The same for a buffer of bytes, whose size the library checks."""
+    import torch
+    return _tensor(t, name, (t.numel(),) if isinstance(t, torch.Tensor) else (), torch.uint8, index)
 
 
 def _block(t, name):
-    """[n][B] of a block of fp32 on the GPU."""
+    """n, B and the GPU of a block."""
     import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != 2:
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
         raise SdnnError(SDNN_EINVAL, f"{name} must be a two-dimensional tensor on the GPU")
-    _tensor(t, name, t.shape, torch.float32, t.device)
-    return t.shape
+    _tensor(t, name, t.shape, torch.float32, t.get_device())
+    n, b = t.shape
+    return n, b, t.get_device()
+
+
+def _elsewhere(index, stream):
+    """None where a call's device is the current one and its stream is the current one; else a context that makes it so, for what the
+    call allocates and launches."""
+    import torch
+    if stream is not None:
+        if stream.device.index != index:
+            raise SdnnError(SDNN_EINVAL, f"the stream is on GPU {stream.device.index}, the tensors on {index}")
+        return torch.cuda.stream(stream)
+    return None if index == torch.cuda.current_device() else torch.cuda.device(index)
 
 
 class Net:
@@ -245,6 +239,7 @@ class Net:
         nbytes = C.c_size_t(0)
         _check(lib().sdnn_workspace_bytes(arr, len(layers), C.byref(self.cfg), C.byref(nbytes)))
         self.device = torch.device(device)
+        self.index = self.device.index if self.device.index is not None else torch.cuda.current_device()
         self.workspace_bytes = nbytes.value
         # the library lays its large arrays out on multiples of up to 2 MiB relative to the workspace: hand it a
         # workspace that starts on a 2 MiB boundary itself (torch only promises 512 bytes)
@@ -297,11 +292,13 @@ class Net:
     def sdnn_backward_input(self, dloss, dx0=None, stream=None):
         """sdnn_backward that also forms dJ/dX_0 [n_in(1)][B], in dx0 if it is given."""
         import torch
-        _tensor(dloss, "dloss", (self.shapes[-1][0], _block(dloss, "dloss")[1]), torch.float32, self.device)
-        shape = (self.shapes[0][1], dloss.shape[1])
-        with _On(self.device, stream) as s:
-            dx0 = self._empty(*shape) if dx0 is None else _tensor(dx0, "dx0", shape, torch.float32, self.device)
-            _check(lib().sdnn_backward_input(self._handle, _dp(dloss), _dp(dx0), s), self._handle)
+        n, b, index = _block(dloss, "dloss")
+        _tensor(dloss, "dloss", (self.shapes[-1][0], b), torch.float32, self.index)
+        if (there := _elsewhere(index, stream)) is not None:
+            with there:
+                return self.sdnn_backward_input(dloss, dx0)
+        dx0 = self._empty(self.shapes[0][1], b) if dx0 is None else _tensor(dx0, "dx0", (self.shapes[0][1], b), torch.float32, index)
+        _check(lib().sdnn_backward_input(self._handle, _dp(dloss), _dp(dx0), _stream_ptr()), self._handle)
         return dx0
 
     def sdnn_sgd_step(self, lr: float, stream=None):
@@ -315,20 +312,20 @@ class Net:
 
     def sdnn_checkpoint_save(self, b: int, ckpt=None, stream=None):
         """The activations of the forward pass of b samples that came last, in 8 bits (in ckpt, a uint8 tensor, if it is given)."""
-        import torch
-        nbytes = self.sdnn_checkpoint_bytes(b)
-        with _On(self.device, stream) as s:
-            if ckpt is None:
-                ckpt = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
-            _tensor(ckpt, "ckpt", (nbytes,), torch.uint8, self.device, least=True)
-            _check(lib().sdnn_checkpoint_save(self._handle, _dp(ckpt), ckpt.numel(), s), self._handle)
+        if (there := _elsewhere(self.index, stream)) is not None:
+            with there:
+                return self.sdnn_checkpoint_save(b, ckpt)
+        if ckpt is None:
+            import torch
+            ckpt = self._empty(self.sdnn_checkpoint_bytes(b), dtype=torch.uint8)
+        _check(lib().sdnn_checkpoint_save(self._handle, _dp(_bytes(ckpt, "ckpt", self.index)), ckpt.numel(), _stream_ptr()), self._handle)
         return ckpt
 
     def sdnn_checkpoint_load(self, ckpt, b: int, stream=None):
-        import torch
-        _tensor(ckpt, "ckpt", (0,), torch.uint8, self.device, least=True)
-        with _On(self.device, stream) as s:
-            _check(lib().sdnn_checkpoint_load(self._handle, _dp(ckpt), ckpt.numel(), int(b), s), self._handle)
+        if (there := _elsewhere(self.index, stream)) is not None:
+            with there:
+                return self.sdnn_checkpoint_load(ckpt, b)
+        _check(lib().sdnn_checkpoint_load(self._handle, _dp(_bytes(ckpt, "ckpt", self.index)), ckpt.numel(), int(b), _stream_ptr()), self._handle)
 
     # -- inspection --
     def _empty(self, *shape, dtype=None):
@@ -401,25 +398,26 @@ class Packed8:
 def sdnn_pack8(x, cap: float = 0.0, packed=None, stream=None) -> Packed8:
     """packed: a uint8 tensor of sdnn_pack8_bytes, or None."""
     import torch
-    n, b = _block(x, "x")
-    nbytes = sdnn_pack8_bytes(n, b)
-    with _On(x.device, stream) as s:
-        if packed is None:
-            packed = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
-        _tensor(packed, "packed", (nbytes,), torch.uint8, x.device, least=True)
-        _check(lib().sdnn_pack8(_dp(x), n, b, cap, _dp(packed), packed.numel(), s))
+    n, b, index = _block(x, "x")
+    if (there := _elsewhere(index, stream)) is not None:
+        with there:
+            return sdnn_pack8(x, cap, packed)
+    if packed is None:
+        packed = torch.empty(sdnn_pack8_bytes(n, b), dtype=torch.uint8, device=x.device)
+    _check(lib().sdnn_pack8(_dp(x), n, b, cap, _dp(_bytes(packed, "packed", index)), packed.numel(), _stream_ptr()))
     return Packed8(packed, n, b, cap)
 
 
 def sdnn_unpack8(packed: Packed8, x=None, stream=None):
     import torch
-    data = packed.data
-    _tensor(data, "packed.data", (0,), torch.uint8, data.device, least=True)
-    with _On(data.device, stream) as s:
-        if x is None:
-            x = torch.empty(packed.n, packed.b, device=data.device)
-        _tensor(x, "x", (packed.n, packed.b), torch.float32, data.device)
-        _check(lib().sdnn_unpack8(_dp(data), data.numel(), packed.n, packed.b, packed.cap, _dp(x), s))
+    index = _bytes(packed.data, "packed.data", packed.data.get_device()).get_device()
+    if (there := _elsewhere(index, stream)) is not None:
+        with there:
+            return sdnn_unpack8(packed, x)
+    if x is None:
+        x = torch.empty(packed.n, packed.b, device=packed.data.device)
+    _tensor(x, "x", (packed.n, packed.b), torch.float32, index)
+    _check(lib().sdnn_unpack8(_dp(packed.data), packed.data.numel(), packed.n, packed.b, packed.cap, _dp(x), _stream_ptr()))
     return x
 
 
@@ -429,54 +427,55 @@ def sdnn_layernorm_workspace_bytes(n: int, b: int) -> int:
     return nbytes.value
 
 
-def _work(work, n, b, device):
+def _work(work, n, b, index):
     import torch
-    nbytes = sdnn_layernorm_workspace_bytes(n, b)
     if work is None:
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return _tensor(work, "work", (nbytes,), torch.uint8, device, least=True)
+        return torch.empty(sdnn_layernorm_workspace_bytes(n, b), dtype=torch.uint8, device=f"cuda:{index}")
+    return _bytes(work, "work", index)
 
 
 def sdnn_layernorm(x, gamma=None, beta=None, eps: float = 1e-5, y=None, stats=None, work=None, stream=None):
     """(y, stats): the block x [n][B] normalized over its rows, and what the backward pass reads, float64 [2][B]."""
     import torch
-    n, b = _block(x, "x")
-    for t, name in ((gamma, "gamma"), (beta, "beta")):
-        if t is not None:
-            _tensor(t, name, (n,), torch.float32, x.device)
-    with _On(x.device, stream) as s:
-        work = _work(work, n, b, x.device)
-        y = torch.empty_like(x) if y is None else _tensor(y, "y", (n, b), torch.float32, x.device)
-        if stats is None:
-            stats = torch.empty(2, b, dtype=torch.float64, device=x.device)
-        _tensor(stats, "stats", (2, b), torch.float64, x.device)
-        _check(lib().sdnn_layernorm(_dp(x), _dp(gamma), _dp(beta), n, b, eps, _dp(y), _dp(stats), _dp(work), work.numel(), s))
+    n, b, index = _block(x, "x")
+    if (there := _elsewhere(index, stream)) is not None:
+        with there:
+            return sdnn_layernorm(x, gamma, beta, eps, y, stats, work)
+    if gamma is not None:
+        _tensor(gamma, "gamma", (n,), torch.float32, index)
+    if beta is not None:
+        _tensor(beta, "beta", (n,), torch.float32, index)
+    work = _work(work, n, b, index)
+    y = torch.empty_like(x) if y is None else _tensor(y, "y", (n, b), torch.float32, index)
+    stats = torch.empty((2, b), dtype=torch.float64, device=x.device) if stats is None else _tensor(stats, "stats", (2, b), torch.float64, index)
+    _check(lib().sdnn_layernorm(_dp(x), _dp(gamma), _dp(beta), n, b, eps, _dp(y), _dp(stats), _dp(work), work.numel(), _stream_ptr()))
     return y, stats
 
 
 def sdnn_layernorm_backward(dy, x, stats, gamma=None, dx=None, dgamma=None, dbeta=None, work=None, stream=None):
     """(dx, dgamma, dbeta).  x: the block that was normalized, or a Packed8 of it; stats: of the forward pass."""
     import torch
-    n, b = _block(dy, "dy")
-    dev = dy.device
+    n, b, index = _block(dy, "dy")
+    if (there := _elsewhere(index, stream)) is not None:
+        with there:
+            return sdnn_layernorm_backward(dy, x, stats, gamma, dx, dgamma, dbeta, work)
     packed = isinstance(x, Packed8)
     if packed:
         if (x.n, x.b) != (n, b):
             raise SdnnError(SDNN_EINVAL, f"x has {x.n} x {x.b} values, dy {n} x {b}")
-        _tensor(x.data, "x.data", (0,), torch.uint8, dev, least=True)
+        _bytes(x.data, "x.data", index)
     else:
-        _tensor(x, "x", (n, b), torch.float32, dev)
-    _tensor(stats, "stats", (2, b), torch.float64, dev)
+        _tensor(x, "x", (n, b), torch.float32, index)
+    _tensor(stats, "stats", (2, b), torch.float64, index)
     if gamma is not None:
-        _tensor(gamma, "gamma", (n,), torch.float32, dev)
-    with _On(dev, stream) as s:
-        work = _work(work, n, b, dev)
-        dx = torch.empty_like(dy) if dx is None else _tensor(dx, "dx", (n, b), torch.float32, dev)
-        dgamma = torch.empty(n, device=dev) if dgamma is None else _tensor(dgamma, "dgamma", (n,), torch.float32, dev)
-        dbeta = torch.empty(n, device=dev) if dbeta is None else _tensor(dbeta, "dbeta", (n,), torch.float32, dev)
-        out = (n, b, _dp(dx), _dp(dgamma), _dp(dbeta), _dp(work), work.numel(), s)
-        if packed:
-            _check(lib().sdnn_layernorm_backward_packed(_dp(dy), _dp(x.data), x.data.numel(), x.cap, _dp(stats), _dp(gamma), *out))
-        else:
-            _check(lib().sdnn_layernorm_backward(_dp(dy), _dp(x), _dp(stats), _dp(gamma), *out))
+        _tensor(gamma, "gamma", (n,), torch.float32, index)
+    work = _work(work, n, b, index)
+    dx = torch.empty_like(dy) if dx is None else _tensor(dx, "dx", (n, b), torch.float32, index)
+    dgamma = dy.new_empty(n) if dgamma is None else _tensor(dgamma, "dgamma", (n,), torch.float32, index)
+    dbeta = dy.new_empty(n) if dbeta is None else _tensor(dbeta, "dbeta", (n,), torch.float32, index)
+    out = (n, b, _dp(dx), _dp(dgamma), _dp(dbeta), _dp(work), work.numel(), _stream_ptr())
+    if packed:
+        _check(lib().sdnn_layernorm_backward_packed(_dp(dy), _dp(x.data), x.data.numel(), x.cap, _dp(stats), _dp(gamma), *out))
+    else:
+        _check(lib().sdnn_layernorm_backward(_dp(dy), _dp(x), _dp(stats), _dp(gamma), *out))
     return dx, dgamma, dbeta
