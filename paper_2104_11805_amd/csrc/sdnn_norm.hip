@@ -17,7 +17,7 @@
 #define NORM_THREADS 512
 #define NORM_ROWS 4
 
-struct __attribute__((packed, aligned(4))) F4 { float v[4]; }; // 16 bytes at any multiple of 4
+typedef float F4 __attribute__((ext_vector_type(4), aligned(4))); // 16 bytes at any multiple of 4
 struct __attribute__((packed, aligned(1))) U1 { unsigned v; }; // 4 bytes anywhere
 
 // A lane's four columns.  They end with the block's last column at the latest: the last lane's first ones may be its neighbour's, and
@@ -38,8 +38,8 @@ template <int CL, bool SMALL> struct Columns {
     __device__ __forceinline__ bool ragged() const { return SMALL || tile0 + 4 * CL > B; } // some lane of the tile is not whole (uniform)
 };
 
-// The block that is normalized, as it is ...
-struct PlainBlock {
+// The block that is normalized, as it is ... (PAST: read past the caches, a block that they do not hold)
+template <bool PAST> struct PlainBlock {
     const float *x;
     struct Raw { float v[4]; };
     template <class C> __device__ __forceinline__ void request(const C &c, size_t row, Raw &t) const
@@ -49,9 +49,9 @@ struct PlainBlock {
 #pragma unroll
             for (int v = 0; v < 4; ++v) t.v[v] = v < c.B ? p[v] : 0.0f;
         } else {
-            const F4 f = *reinterpret_cast<const F4 *>(p);
+            const F4 f = PAST ? __builtin_nontemporal_load(reinterpret_cast<const F4 *>(p)) : *reinterpret_cast<const F4 *>(p);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) t.v[v] = f.v[v];
+            for (int v = 0; v < 4; ++v) t.v[v] = f[v];
         }
     }
     __device__ __forceinline__ void values(const Raw &t, float (&x4)[4]) const
@@ -184,16 +184,16 @@ __device__ __forceinline__ bool find_tile(const NormArgs &a, int splits, int &ti
 
 // part [range][B]: sums of x - x0 and of its square, x0 the sample's first value: nothing cancels where the mean is large.
 // firsts [B]: x0, which the second launch may write its results over.
-template <int CL, bool SMALL>
+template <int CL, bool SMALL, bool PAST>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restrict__ x, const NormArgs a, double2 *__restrict__ part, float *__restrict__ firsts)
 {
     int tile, range, r0, r1;
     if (!find_tile(a, 1, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
-    const PlainBlock in{x};
+    const PlainBlock<PAST> in{x};
     double s1[4] = {}, s2[4] = {};
     if (c.any()) {
-        PlainBlock::Raw first, t[NORM_ROWS];
+        typename PlainBlock<PAST>::Raw first, t[NORM_ROWS];
         in.request(c, 0, first);
         if (range == 0 && (int)threadIdx.x < CL)
 #pragma unroll
@@ -220,10 +220,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restr
 template <class C> __device__ __forceinline__ void store_row(const C &c, float *p, const float (&o)[4])
 {
     if (c.whole()) {
-        F4 f;
-#pragma unroll
-        for (int v = 0; v < 4; ++v) f.v[v] = o[v];
-        *reinterpret_cast<F4 *>(p) = f;
+        __builtin_nontemporal_store(F4{o[0], o[1], o[2], o[3]}, reinterpret_cast<F4 *>(p));
     } else {
 #pragma unroll
         for (int v = 0; v < 4; ++v)
@@ -231,7 +228,7 @@ template <class C> __device__ __forceinline__ void store_row(const C &c, float *
     }
 }
 
-template <int CL, bool SMALL>
+template <int CL, bool SMALL, bool PAST>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, const float *__restrict__ gamma, const float *__restrict__ beta, const NormArgs a,
                                                              double eps, const double2 *__restrict__ part, const float *__restrict__ firsts, float *y,
                                                              double *__restrict__ stats)
@@ -239,9 +236,9 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
     int tile, range, r0, r1;
     if (!find_tile(a, a.splits, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
-    const PlainBlock in{x};
+    const PlainBlock<PAST> in{x};
     struct Rows {
-        PlainBlock::Raw t[NORM_ROWS];
+        typename PlainBlock<PAST>::Raw t[NORM_ROWS];
         float g[NORM_ROWS], b[NORM_ROWS];
     } now, next;
     auto request = [&](int r, Rows &w) {
@@ -315,7 +312,7 @@ struct RowSums {
 
 // part [range][B]: sums of g dY and of g dY h over the rows of a range, h = (x - mean) rstd; and the sums of dY h and dY over the
 // tile's columns.
-template <int CL, bool SMALL, class Block>
+template <int CL, bool SMALL, bool PAST, class Block>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__restrict__ dy, const Block x, const double *__restrict__ stats,
                                                                  const float *__restrict__ gamma, const NormArgs a, double2 *__restrict__ part, const RowSums rs)
 {
@@ -324,7 +321,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
     int tile, range, r0, r1;
     if (!find_tile(a, 1, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
-    const PlainBlock up{dy};
+    const PlainBlock<PAST> up{dy};
     double p[4] = {}, q[4] = {}, mean[4] = {}, rstd[4] = {};
 #pragma unroll
     for (int v = 0; v < 4; ++v)
@@ -333,7 +330,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
             rstd[v] = stats[a.B + c.base + v];
         }
     for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r)) {
-        PlainBlock::Raw d[NORM_ROWS];
+        typename PlainBlock<PAST>::Raw d[NORM_ROWS];
         typename Block::Raw t[NORM_ROWS];
         float g[NORM_ROWS];
 #pragma unroll
@@ -382,7 +379,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
 }
 
 // rs.part: not NULL in the last launch over the tiles of a block with more than one across.
-template <int CL, bool SMALL, class Block>
+template <int CL, bool SMALL, bool PAST, class Block>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_apply(const float *dy, const Block x, const double *__restrict__ stats, const float *__restrict__ gamma,
                                                                   const NormArgs a, const double2 *__restrict__ part, float *dx, const RowSums rs)
 {
@@ -400,9 +397,9 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_apply(const float *d
     }
     if (!dx) return;
     const Columns<CL, SMALL> c(tile, a.B);
-    const PlainBlock up{dy};
+    const PlainBlock<PAST> up{dy};
     struct Rows {
-        PlainBlock::Raw d[NORM_ROWS];
+        typename PlainBlock<PAST>::Raw d[NORM_ROWS];
         typename Block::Raw t[NORM_ROWS];
         float g[NORM_ROWS];
     } now, next;
@@ -452,6 +449,7 @@ static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 struct NormPlan {
     NormArgs a;
     int cl;
+    bool past;
     size_t row_part, firsts, total; // bytes into the workspace
 };
 static NormPlan plan_norm(int n, int B)
@@ -459,6 +457,7 @@ static NormPlan plan_norm(int n, int B)
     NormPlan p;
     NormArgs &a = p.a;
     a.n = n; a.B = B;
+    p.past = (int64_t)n * B >= (int64_t)48 << 20;
     const int most = std::max(1, (int)std::sqrt(n / 4.0)); // the second launch reads 16 bytes per range and column, and 4 per row
     int unit;
     for (p.cl = across(B);; p.cl /= 2) { // narrower tiles where there would be few
@@ -503,15 +502,14 @@ extern "C" int sdnn_layernorm_workspace_bytes(int32_t n, int32_t B, size_t *byte
     return SDNN_OK;
 }
 
-template <int CL, bool SMALL>
+template <int CL, bool SMALL, bool PAST>
 static int forward(const float *x, const float *gamma, const float *beta, double eps, float *y, double *stats, void *work, const NormPlan &pl, hipStream_t stream)
 {
     double2 *part = (double2 *)work;
     float *firsts = (float *)((char *)work + pl.firsts);
     const NormArgs &a = pl.a;
-    hipLaunchKernelGGL((k_norm_sums<CL, SMALL>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
-    hipLaunchKernelGGL((k_norm_apply<CL, SMALL>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts,
-                       y, stats);
+    hipLaunchKernelGGL((k_norm_sums<CL, SMALL, PAST>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
+    hipLaunchKernelGGL((k_norm_apply<CL, SMALL, PAST>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts, y, stats);
     return sdnn_launched();
 }
 
@@ -525,41 +523,48 @@ extern "C" int sdnn_layernorm(const float *d_X, const float *d_gamma, const floa
     const NormPlan pl = plan_norm(n, B);
     hipStream_t stream = (hipStream_t)stream_;
     switch (pl.cl) {
-    case 1: return forward<1, true>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    case 4: return forward<4, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    case 8: return forward<8, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    case 16: return forward<16, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    case 32: return forward<32, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    default: return forward<64, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 1: return forward<1, true, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 4: return forward<4, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 8: return forward<8, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 16: return forward<16, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 32: return forward<32, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    default:
+        if (pl.past) return forward<64, false, true>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+        return forward<64, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
     }
 }
 
-template <int CL, bool SMALL, class Block>
+template <int CL, bool SMALL, bool PAST, class Block>
 static int backward(const float *dy, const Block &x, const double *stats, const float *gamma, float *dx, RowSums rs, void *work, const NormPlan &pl, hipStream_t stream)
 {
     double2 *part = (double2 *)work;
     const NormArgs &a = pl.a;
     rs.part = a.tiles > 1 ? (double *)((char *)work + pl.row_part) : nullptr;
-    hipLaunchKernelGGL((k_norm_grad_sums<CL, SMALL, Block>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, rs);
+    hipLaunchKernelGGL((k_norm_grad_sums<CL, SMALL, PAST, Block>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, rs);
     if (dx || rs.part)
-        hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma,
-                           a, part, dx, rs);
+        hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, PAST, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, dx, rs);
     return sdnn_launched();
 }
-template <class Block>
-static int backward_any(const float *dy, const Block &x, const double *stats, const float *gamma, int n, int B, float *dx, float *dgamma, float *dbeta, void *work,
-                        void *stream_)
+template <bool PACKED>
+static int backward_any(const float *dy, const float *x, const PackedBlock &x8, const double *stats, const float *gamma, int n, int B, float *dx, float *dgamma,
+                        float *dbeta, void *work, void *stream_)
 {
     const NormPlan pl = plan_norm(n, B);
     const RowSums rs{nullptr, dgamma, dbeta};
     hipStream_t stream = (hipStream_t)stream_;
+    auto go = [&](auto cl, auto small, auto past) {
+        if constexpr (PACKED) return backward<cl.value, small.value, past.value>(dy, x8, stats, gamma, dx, rs, work, pl, stream);
+        else return backward<cl.value, small.value, past.value>(dy, PlainBlock<past.value>{x}, stats, gamma, dx, rs, work, pl, stream);
+    };
+    const std::integral_constant<bool, true> yes;
+    const std::integral_constant<bool, false> no;
     switch (pl.cl) {
-    case 1: return backward<1, true>(dy, x, stats, gamma, dx, rs, work, pl, stream);
-    case 4: return backward<4, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
-    case 8: return backward<8, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
-    case 16: return backward<16, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
-    case 32: return backward<32, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
-    default: return backward<64, false>(dy, x, stats, gamma, dx, rs, work, pl, stream);
+    case 1: return go(std::integral_constant<int, 1>(), yes, no);
+    case 4: return go(std::integral_constant<int, 4>(), no, no);
+    case 8: return go(std::integral_constant<int, 8>(), no, no);
+    case 16: return go(std::integral_constant<int, 16>(), no, no);
+    case 32: return go(std::integral_constant<int, 32>(), no, no);
+    default: return pl.past ? go(std::integral_constant<int, 64>(), no, yes) : go(std::integral_constant<int, 64>(), no, no);
     }
 }
 
@@ -577,7 +582,7 @@ extern "C" int sdnn_layernorm_backward(const float *d_dY, const float *d_X, cons
     if (!rc) rc = check_backward(d_dY, d_stats, d_dX, d_dgamma, d_dbeta);
     if (rc) return rc;
     if (!d_X) return sdnn_fail(SDNN_EINVAL, "d_X is NULL");
-    return backward_any(d_dY, PlainBlock{d_X}, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
+    return backward_any<false>(d_dY, d_X, PackedBlock(), d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
 }
 
 extern "C" int sdnn_layernorm_backward_packed(const float *d_dY, const void *d_packed, size_t packed_bytes, float cap, const double *d_stats,
@@ -592,5 +597,5 @@ extern "C" int sdnn_layernorm_backward_packed(const float *d_dY, const void *d_p
     x.codes = (const uint8_t *)d_packed;
     x.scales = (const uint16_t *)(x.codes + PACK_GROUP * pack8_groups((int64_t)n * B));
     x.cap = cap; x.below = nextafterf(cap, 0.0f);
-    return backward_any(d_dY, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
+    return backward_any<true>(d_dY, nullptr, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
 }
