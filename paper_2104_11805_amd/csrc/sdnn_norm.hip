@@ -24,14 +24,19 @@ struct __attribute__((packed, aligned(1))) U1 { unsigned v; }; // 4 bytes anywhe
 // are left out of everything.  SMALL: B < 4, one lane across.
 template <int CL, bool SMALL> struct Columns {
     static constexpr bool small = SMALL;
-    int tile0, base, first, B; // columns base .. base + 3, of which those from `first` on are the lane's own; none if first >= B
+    int tile0, B, lane_row;    // lane_row: of the rows that the wavefront has at a time
+    int base, first;           // columns base .. base + 3, of which those from `first` on are the lane's own; none if first >= B
     __device__ __forceinline__ Columns(int tile, int B_)
     {
         B = B_;
         tile0 = tile * 4 * CL;
         first = tile0 + 4 * (int)(threadIdx.x & (CL - 1));
         base = SMALL ? 0 : min(first, B - 4);
+        lane_row = (int)(threadIdx.x & 63) / CL;
     }
+    __device__ __forceinline__ unsigned at() const { return (unsigned)(lane_row * B + base); } // from the start of the wavefront's first row
+
+    template <class T> __device__ __forceinline__ T *in(T *p) const { return (T *)((uintptr_t)p + 4u * at()); } // (32 bits beside a uniform address)
     __device__ __forceinline__ bool any() const { return first < B; }
     __device__ __forceinline__ bool whole() const { return !SMALL && base == first; }
     __device__ __forceinline__ bool own(int v) const { return SMALL ? v < B : base + v >= first; }
@@ -42,9 +47,10 @@ template <int CL, bool SMALL> struct Columns {
 template <bool PAST> struct PlainBlock {
     const float *x;
     struct Raw { float v[4]; };
-    template <class C> __device__ __forceinline__ void request(const C &c, size_t row, Raw &t) const
+    // start: of the wavefront's first row
+    template <class C> __device__ __forceinline__ void request(const C &c, size_t start, Raw &t) const
     {
-        const float *p = x + row * (size_t)c.B + c.base;
+        const float *p = c.in(x + start);
         if constexpr (C::small) {
 #pragma unroll
             for (int v = 0; v < 4; ++v) t.v[v] = v < c.B ? p[v] : 0.0f;
@@ -54,36 +60,44 @@ template <bool PAST> struct PlainBlock {
             for (int v = 0; v < 4; ++v) t.v[v] = f[v];
         }
     }
-    __device__ __forceinline__ void values(const Raw &t, float (&x4)[4]) const
+    template <class C> __device__ __forceinline__ void values(const C &, const Raw &t, float (&x4)[4]) const
     {
 #pragma unroll
         for (int v = 0; v < 4; ++v) x4[v] = t.v[v];
     }
 };
-// ... or in 8 bits: four codes, and the scales of the first and the last of them
-struct PackedBlock {
+// ... or in 8 bits: four codes, and the scales of the first and the last of them (the same where rows are whole fours)
+struct PackedArgs {
     const uint8_t *codes;
     const uint16_t *scales;
     float cap, below;
+};
+template <bool SIGNED> struct PackedBlock : PackedArgs {
     struct Raw { unsigned code; float scale[2]; int place; };
-    template <class C> __device__ __forceinline__ void request(const C &c, size_t row, Raw &t) const
+    template <class C> __device__ __forceinline__ void request(const C &c, size_t start, Raw &t) const
     {
-        const size_t e = row * (size_t)c.B + c.base;
         const int last = C::small ? c.B - 1 : 3;
+        const uint8_t *code = codes + start + c.at();
+        const unsigned at = (unsigned)(start % PACK_GROUP) + c.at(); // from the first row's first group on
+        const uint16_t *scale = scales + start / PACK_GROUP;
         if constexpr (C::small) {
-            t.code = codes[e];
-            for (int v = 1; v <= last; ++v) t.code |= (unsigned)codes[e + v] << (8 * v);
+            t.code = code[0];
+            for (int v = 1; v <= last; ++v) t.code |= (unsigned)code[v] << (8 * v);
         } else {
-            t.code = reinterpret_cast<const U1 *>(codes + e)->v;
+            t.code = reinterpret_cast<const U1 *>(code)->v;
         }
-        t.place = (int)(e % PACK_GROUP);
-        t.scale[0] = __uint_as_float((unsigned)scales[e / PACK_GROUP] << 16);
-        t.scale[1] = __uint_as_float((unsigned)scales[(e + last) / PACK_GROUP] << 16);
+        t.place = (int)(at % PACK_GROUP);
+        t.scale[0] = __uint_as_float((unsigned)scale[at / PACK_GROUP] << 16);
+        if (c.B & 3) t.scale[1] = __uint_as_float((unsigned)scale[(at + last) / PACK_GROUP] << 16);
     }
-    __device__ __forceinline__ void values(const Raw &t, float (&x4)[4]) const
+    template <class C> __device__ __forceinline__ void values(const C &c, const Raw &t, float (&x4)[4]) const
     {
+        float scale[4] = {t.scale[0], t.scale[0], t.scale[0], t.scale[0]};
+        if (c.B & 3)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) x4[v] = pack8_value(t.code >> (8 * v) & 255u, t.place + v < PACK_GROUP ? t.scale[0] : t.scale[1], cap, below);
+            for (int v = 1; v < 4; ++v) scale[v] = t.place + v < PACK_GROUP ? t.scale[0] : t.scale[1];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) x4[v] = pack8_value_of<SIGNED>(t.code >> (8 * v) & 255u, scale[v], cap, below);
     }
 };
 
@@ -123,30 +137,35 @@ __device__ __forceinline__ void store_column_sums(const C &c, const double (&a)[
     }
 }
 
-// The sums of all ranges for the tile's columns, put through `finish`; the results for the lane's columns.
+// The sums of all ranges for the tile's columns, put through `finish`; the results for the lane's columns.  ready: there they are.
 template <int CL, class C, class F>
-__device__ __forceinline__ void load_column_sums(const C &c, const double2 *__restrict__ part, int ranges, double (&a)[4], double (&b)[4], F finish)
+__device__ __forceinline__ void load_column_sums(const C &c, const double2 *__restrict__ part, int ranges, const double2 *__restrict__ ready, double (&a)[4],
+                                                 double (&b)[4], F finish)
 {
     constexpr int CT = 4 * CL, K = NORM_THREADS / CT;
     __shared__ double2 lds[NORM_THREADS];
     const int tid = threadIdx.x, col = c.tile0 + (tid & (CT - 1));
-    double2 s = make_double2(0.0, 0.0);
-    if (col < c.B)
+    if (ready) {
+        if (tid < CT && col < c.B) lds[tid] = ready[col];
+    } else {
+        double2 s = make_double2(0.0, 0.0);
+        if (col < c.B)
 #pragma unroll 8
-        for (int k = tid / CT; k < ranges; k += K) {
-            const double2 t = part[(size_t)k * c.B + col];
-            s.x += t.x;
-            s.y += t.y;
-        }
-    lds[tid] = s;
-    __syncthreads();
-    if (tid < CT) {
-        for (int k = 1; k < K; ++k) {
-            s.x += lds[k * CT + tid].x;
-            s.y += lds[k * CT + tid].y;
-        }
-        if (col < c.B) s = finish(col, s);
+            for (int k = tid / CT; k < ranges; k += K) {
+                const double2 t = part[(size_t)k * c.B + col];
+                s.x += t.x;
+                s.y += t.y;
+            }
         lds[tid] = s;
+        __syncthreads();
+        if (tid < CT) {
+            for (int k = 1; k < K; ++k) {
+                s.x += lds[k * CT + tid].x;
+                s.y += lds[k * CT + tid].y;
+            }
+            if (col < c.B) s = finish(col, s);
+            lds[tid] = s;
+        }
     }
     __syncthreads();
 #pragma unroll
@@ -157,15 +176,62 @@ __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__re
     }
 }
 
-// The rows that a thread walks: its first one, and NORM_ROWS of them at a time, row_of<CL>(r, u), of those below r1.
-template <int CL> __device__ __forceinline__ int first_row(int r0) { return r0 + (int)threadIdx.x / CL; }
+// The rows that a wavefront walks: from its first one on 64 / CL at a time, the lane's is lane_row further, and NORM_ROWS times that, row_of<CL>(r,
+// u), are requested together.  r and where that row starts, e, are the same for the wavefront.
+template <int CL> __device__ __forceinline__ int first_row(int r0) { return r0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * (64 / CL); }
 template <int CL> __device__ __forceinline__ int row_of(int r, int u) { return r + u * (NORM_THREADS / CL); }
 template <int CL> __device__ __forceinline__ int next_rows(int r) { return row_of<CL>(r, NORM_ROWS); }
+template <class C> __device__ __forceinline__ size_t first_start(const C &c, int r) { return (size_t)r * (size_t)c.B; }
+template <int CL, class C> __device__ __forceinline__ size_t start_of(const C &c, size_t e, int u) { return e + (size_t)u * (NORM_THREADS / CL) * (size_t)c.B; }
+template <int CL, class C> __device__ __forceinline__ size_t next_start(const C &c, size_t e) { return start_of<CL>(c, e, NORM_ROWS); }
 
 struct NormArgs {
     int32_t n, B, rows;            // rows of a range
     int32_t tiles, ranges, splits; // tiles across; ranges; second launches: parts of a range
+    double2 *ready;                // NULL, or [B]: the ranges' sums are added up by a launch between the two (k_norm_finish)
 };
+
+// A sample's mean and 1/sqrt(variance + eps) from its sums; an infinity or NaN in a sample: NaN, and so is all of its result.
+__device__ __forceinline__ double2 statistics(double2 s, float first, double inv, double eps)
+{
+    const double m = s.x * inv, var = s.y * inv - m * m;
+    return make_double2((double)first + m, 1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));
+}
+
+// stats: forward, [2][B] or NULL; firsts: forward, NULL: back.
+#define FINISH_COLUMNS 16
+__global__ void __launch_bounds__(512) k_norm_finish(const NormArgs a, const double2 *__restrict__ part, const float *__restrict__ firsts, double eps, double *__restrict__ stats)
+{
+    __shared__ double2 lds[512];
+    const int tid = threadIdx.x, col = (int)blockIdx.x * FINISH_COLUMNS + (tid & (FINISH_COLUMNS - 1));
+    double2 s = make_double2(0.0, 0.0);
+    if (col < a.B)
+#pragma unroll 8
+        for (int k = tid / FINISH_COLUMNS; k < a.ranges; k += 512 / FINISH_COLUMNS) {
+            const double2 t = part[(size_t)k * a.B + col];
+            s.x += t.x;
+            s.y += t.y;
+        }
+    lds[tid] = s;
+    __syncthreads();
+    if (tid >= FINISH_COLUMNS || col >= a.B) return;
+#pragma unroll 8
+    for (int k = FINISH_COLUMNS + tid; k < 512; k += FINISH_COLUMNS) {
+        s.x += lds[k].x;
+        s.y += lds[k].y;
+    }
+    const double inv = 1.0 / (double)a.n;
+    if (firsts) {
+        s = statistics(s, firsts[col], inv, eps);
+        if (stats) {
+            stats[col] = s.x;
+            stats[a.B + col] = s.y;
+        }
+    } else {
+        s = make_double2(s.x * inv, s.y * inv);
+    }
+    a.ready[col] = s;
+}
 // Which part a workgroup takes.  Workgroup ids go round the XCDs: an XCD takes whole rows of the block (a tile's columns of all rows lie
 // in the same few of an L2's channels), and in the second launch those that it had in the first.  Few ranges: any.
 __device__ __forceinline__ bool find_tile(const NormArgs &a, int splits, int &tile, int &range, int &r0, int &r1)
@@ -194,18 +260,20 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restr
     double s1[4] = {}, s2[4] = {};
     if (c.any()) {
         typename PlainBlock<PAST>::Raw first, t[NORM_ROWS];
-        in.request(c, 0, first);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) first.v[v] = x[min(c.base + v, a.B - 1)];
         if (range == 0 && (int)threadIdx.x < CL)
 #pragma unroll
             for (int v = 0; v < 4; ++v)
                 if (c.own(v)) firsts[c.base + v] = first.v[v];
-        for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r)) {
+        size_t e = first_start(c, first_row<CL>(r0));
+        for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r), e = next_start<CL>(c, e)) {
 #pragma unroll
             for (int u = 0; u < NORM_ROWS; ++u)
-                if (row_of<CL>(r, u) < r1) in.request(c, row_of<CL>(r, u), t[u]);
+                if (row_of<CL>(r, u) + c.lane_row < r1) in.request(c, start_of<CL>(c, e, u), t[u]);
 #pragma unroll
             for (int u = 0; u < NORM_ROWS; ++u)
-                if (row_of<CL>(r, u) < r1)
+                if (row_of<CL>(r, u) + c.lane_row < r1)
 #pragma unroll
                     for (int v = 0; v < 4; ++v) {
                         const double d = (double)t[u].v[v] - (double)first.v[v];
@@ -240,39 +308,41 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
     struct Rows {
         typename PlainBlock<PAST>::Raw t[NORM_ROWS];
         float g[NORM_ROWS], b[NORM_ROWS];
-    } now, next;
-    auto request = [&](int r, Rows &w) {
+    } now;
+    auto request = [&](int r, size_t e, Rows &w) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) < r1 && c.any()) {
-                in.request(c, row_of<CL>(r, u), w.t[u]);
-                w.g[u] = gamma ? gamma[row_of<CL>(r, u)] : 1.0f;
-                w.b[u] = beta ? beta[row_of<CL>(r, u)] : 0.0f;
+            if (row_of<CL>(r, u) + c.lane_row < r1 && c.any()) {
+                in.request(c, start_of<CL>(c, e, u), w.t[u]);
+                w.g[u] = gamma ? gamma[row_of<CL>(r, u) + c.lane_row] : 1.0f;
+                w.b[u] = beta ? beta[row_of<CL>(r, u) + c.lane_row] : 0.0f;
             }
     };
     int r = first_row<CL>(r0);
-    request(r, now); // on their way while the sums are added up
+    size_t e = first_start(c, r);
+    request(r, e, now); // on their way while the sums are added up
     double mean[4], rstd[4];
     const double inv = 1.0 / (double)a.n;
-    load_column_sums<CL>(c, part, a.ranges, mean, rstd, [&](int col, double2 s) {
-        const double m = s.x * inv, var = s.y * inv - m * m;
-        const double2 out = make_double2((double)firsts[col] + m, 1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps)); // an infinity or NaN in a sample: NaN, and
-        if (r0 == 0 && stats) {                                                                              // so is all of its result
+    load_column_sums<CL>(c, part, a.ranges, a.ready, mean, rstd, [&](int col, double2 s) {
+        const double2 out = statistics(s, firsts[col], inv, eps);
+        if (r0 == 0 && stats) {
             stats[col] = out.x;
             stats[a.B + col] = out.y;
         }
         return out;
     });
     if (!c.any()) return;
-    for (; r < r1; r = next_rows<CL>(r), now = next) {
-        request(next_rows<CL>(r), next);
+    double shift[4]; // h = (x - mean) rstd as x rstd + shift
+#pragma unroll
+    for (int v = 0; v < 4; ++v) shift[v] = -mean[v] * rstd[v];
+    for (; r < r1; r = next_rows<CL>(r), e = next_start<CL>(c, e), request(r, e, now)) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) < r1) {
+            if (row_of<CL>(r, u) + c.lane_row < r1) {
                 float o[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) o[v] = (float)fma(((double)now.t[u].v[v] - mean[v]) * rstd[v], (double)now.g[u], (double)now.b[u]);
-                store_row(c, y + (size_t)row_of<CL>(r, u) * a.B + c.base, o);
+                for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)now.t[u].v[v], rstd[v], shift[v]), (double)now.g[u], (double)now.b[u]);
+                store_row(c, c.in(y + start_of<CL>(c, e, u)), o);
             }
     }
 }
@@ -313,7 +383,7 @@ struct RowSums {
 // part [range][B]: sums of g dY and of g dY h over the rows of a range, h = (x - mean) rstd; and the sums of dY h and dY over the
 // tile's columns.
 template <int CL, bool SMALL, bool PAST, class Block>
-__global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__restrict__ dy, const Block x, const double *__restrict__ stats,
+__global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float *__restrict__ dy, const Block x, const double *__restrict__ stats,
                                                                  const float *__restrict__ gamma, const NormArgs a, double2 *__restrict__ part, const RowSums rs)
 {
     static_assert(NORM_ROWS == 4, "eight sums at a time");
@@ -322,38 +392,38 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
     if (!find_tile(a, 1, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
     const PlainBlock<PAST> up{dy};
-    double p[4] = {}, q[4] = {}, mean[4] = {}, rstd[4] = {};
+    double p[4] = {}, q[4] = {}, shift[4] = {}, rstd[4] = {}; // h = (x - mean) rstd as x rstd + shift
 #pragma unroll
     for (int v = 0; v < 4; ++v)
         if (c.any() && c.own(v)) {
-            mean[v] = stats[c.base + v];
             rstd[v] = stats[a.B + c.base + v];
+            shift[v] = -stats[c.base + v] * rstd[v];
         }
-    for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r)) {
+    size_t e = first_start(c, first_row<CL>(r0));
+    for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r), e = next_start<CL>(c, e)) {
         typename PlainBlock<PAST>::Raw d[NORM_ROWS];
         typename Block::Raw t[NORM_ROWS];
         float g[NORM_ROWS];
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) < r1 && c.any()) {
-                const size_t row = (size_t)row_of<CL>(r, u);
-                up.request(c, row, d[u]);
-                x.request(c, row, t[u]);
-                g[u] = gamma ? gamma[row] : 1.0f;
+            if (row_of<CL>(r, u) + c.lane_row < r1 && c.any()) {
+                up.request(c, start_of<CL>(c, e, u), d[u]);
+                x.request(c, start_of<CL>(c, e, u), t[u]);
+                g[u] = gamma ? gamma[row_of<CL>(r, u) + c.lane_row] : 1.0f;
             }
         double sum[8] = {};
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) < r1 && c.any()) {
+            if (row_of<CL>(r, u) + c.lane_row < r1 && c.any()) {
                 float xv[4];
-                x.values(t[u], xv);
+                x.values(c, t[u], xv);
                 if (c.ragged())
 #pragma unroll
                     for (int v = 0; v < 4; ++v)
                         if (!c.own(v)) d[u].v[v] = xv[v] = 0.0f;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const double h = ((double)xv[v] - mean[v]) * rstd[v], dv = (double)d[u].v[v], gd = (double)g[u] * dv;
+                    const double h = fma((double)xv[v], rstd[v], shift[v]), dv = (double)d[u].v[v], gd = (double)g[u] * dv;
                     p[v] += gd;
                     q[v] = fma(gd, h, q[v]);
                     sum[2 * u] = fma(dv, h, sum[2 * u]);
@@ -367,7 +437,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
 #pragma unroll
             for (int j = 0; j < n_sums; ++j) {
                 const int u = (first + j) >> 1, w = (first + j) & 1;
-                const size_t row = (size_t)row_of<CL>(r, u);
+                const size_t row = (size_t)(row_of<CL>(r, u) + c.lane_row);
                 if (row < (size_t)r1) {
                     if (rs.part) rs.part[2 * ((size_t)tile * a.n + row) + w] = sum[j];
                     else if (w == 0 && rs.dgamma) rs.dgamma[row] = (float)sum[j];
@@ -380,19 +450,19 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_sums(const float *__
 
 // rs.part: not NULL in the last launch over the tiles of a block with more than one across.
 template <int CL, bool SMALL, bool PAST, class Block>
-__global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_apply(const float *dy, const Block x, const double *__restrict__ stats, const float *__restrict__ gamma,
+__global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float *dy, const Block x, const double *__restrict__ stats, const float *__restrict__ gamma,
                                                                   const NormArgs a, const double2 *__restrict__ part, float *dx, const RowSums rs)
 {
     int tile, range, r0, r1;
     if (!find_tile(a, a.splits, tile, range, r0, r1)) return;
     if (rs.part) { // the rows' sums: every tile across adds up a share of the range's
-        const int share = (r1 - r0 + a.tiles - 1) / a.tiles, e1 = 2 * min(r1, r0 + (tile + 1) * share);
-        for (int e = 2 * (r0 + tile * share) + (int)threadIdx.x; e < e1; e += NORM_THREADS) {
+        const int share = (r1 - r0 + a.tiles - 1) / a.tiles, end = 2 * min(r1, r0 + (tile + 1) * share);
+        for (int i = 2 * (r0 + tile * share) + (int)threadIdx.x; i < end; i += NORM_THREADS) {
             double s = 0.0;
 #pragma unroll 4
-            for (int k = 0; k < a.tiles; ++k) s += rs.part[2 * (size_t)k * a.n + e];
-            float *out = e & 1 ? rs.dbeta : rs.dgamma;
-            if (out) out[e >> 1] = (float)s;
+            for (int k = 0; k < a.tiles; ++k) s += rs.part[2 * (size_t)k * a.n + i];
+            float *out = i & 1 ? rs.dbeta : rs.dgamma;
+            if (out) out[i >> 1] = (float)s;
         }
     }
     if (!dx) return;
@@ -402,41 +472,41 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_grad_apply(const float *d
         typename PlainBlock<PAST>::Raw d[NORM_ROWS];
         typename Block::Raw t[NORM_ROWS];
         float g[NORM_ROWS];
-    } now, next;
-    auto request = [&](int r, Rows &w) {
+    } now;
+    auto request = [&](int r, size_t e, Rows &w) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) < r1 && c.any()) {
-                up.request(c, row_of<CL>(r, u), w.d[u]);
-                x.request(c, row_of<CL>(r, u), w.t[u]);
-                w.g[u] = gamma ? gamma[row_of<CL>(r, u)] : 1.0f;
+            if (row_of<CL>(r, u) + c.lane_row < r1 && c.any()) {
+                up.request(c, start_of<CL>(c, e, u), w.d[u]);
+                x.request(c, start_of<CL>(c, e, u), w.t[u]);
+                w.g[u] = gamma ? gamma[row_of<CL>(r, u) + c.lane_row] : 1.0f;
             }
     };
     int r = first_row<CL>(r0);
-    request(r, now); // on their way while the sums are added up
-    double p[4], q[4], mean[4] = {}, rstd[4] = {};
+    size_t e = first_start(c, r);
+    request(r, e, now); // on their way while the sums are added up
+    double p[4], q[4], rstd[4] = {}; // dX = (g rstd) dY - p - q x: p and q become those constants of a column
     const double inv = 1.0 / (double)a.n;
-    load_column_sums<CL>(c, part, a.ranges, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
+    load_column_sums<CL>(c, part, a.ranges, a.ready, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
     if (!c.any()) return;
 #pragma unroll
     for (int v = 0; v < 4; ++v)
         if (c.own(v)) {
-            mean[v] = stats[c.base + v];
-            rstd[v] = stats[a.B + c.base + v];
+            const double r = stats[a.B + c.base + v], t = r * q[v];
+            rstd[v] = r;
+            p[v] = fma(-stats[c.base + v] * r, t, r * p[v]);
+            q[v] = r * t;
         }
-    for (; r < r1; r = next_rows<CL>(r), now = next) {
-        request(next_rows<CL>(r), next);
+    for (; r < r1; r = next_rows<CL>(r), e = next_start<CL>(c, e), request(r, e, now)) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) < r1) {
+            if (row_of<CL>(r, u) + c.lane_row < r1) {
                 float xv[4], o[4];
-                x.values(now.t[u], xv);
+                x.values(c, now.t[u], xv);
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    const double h = ((double)xv[v] - mean[v]) * rstd[v];
-                    o[v] = (float)(rstd[v] * fma(-h, q[v], fma((double)now.g[u], (double)now.d[u].v[v], -p[v])));
-                }
-                store_row(c, dx + (size_t)row_of<CL>(r, u) * a.B + c.base, o);
+                for (int v = 0; v < 4; ++v)
+                    o[v] = (float)fma((double)now.g[u] * rstd[v], (double)now.d[u].v[v], -fma(q[v], (double)xv[v], p[v]));
+                store_row(c, c.in(dx + start_of<CL>(c, e, u)), o);
             }
     }
 }
@@ -446,11 +516,16 @@ static int across(int B) { return B < 4 ? 1 : B <= 16 ? 4 : B <= 32 ? 8 : B <= 6
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Tiles: enough workgroups to fill the chip, but not so many ranges that their sums are a load to add up.
+// From so many values on, the ranges' sums are added up by a launch of their own (4 us); below, every workgroup of the second launch does
+// so for its columns, of fewer ranges.
+#ifndef FINISH_COUNT
+#define FINISH_COUNT (1 << 22)
+#endif
 struct NormPlan {
     NormArgs a;
     int cl;
     bool past;
-    size_t row_part, firsts, total; // bytes into the workspace
+    size_t row_part, firsts, ready, total; // bytes into the workspace; ready 0: there is none
 };
 static NormPlan plan_norm(int n, int B)
 {
@@ -458,20 +533,28 @@ static NormPlan plan_norm(int n, int B)
     NormArgs &a = p.a;
     a.n = n; a.B = B;
     p.past = (int64_t)n * B >= (int64_t)48 << 20;
-    const int most = std::max(1, (int)std::sqrt(n / 4.0)); // the second launch reads 16 bytes per range and column, and 4 per row
+    const bool finish = (int64_t)n * B >= FINISH_COUNT;
     int unit;
-    for (p.cl = across(B);; p.cl /= 2) { // narrower tiles where there would be few
+    for (p.cl = across(B);; p.cl /= 2) {
         unit = NORM_ROWS * NORM_THREADS / p.cl;
         a.tiles = ceil_div(B, 4 * p.cl);
-        a.rows = std::max(unit, ceil_div(ceil_div(n, std::max(1, std::min(most, 1024 / a.tiles))), unit) * unit);
+        // without that launch: 16 bytes per range and column against 4 per row, and narrower tiles where there would be few
+        const int most = finish ? std::max(1, 512 / a.tiles) : std::max(1, std::min((int)std::sqrt(n / 4.0), 512 / a.tiles));
+        a.rows = std::max(unit, ceil_div(ceil_div(n, most), unit) * unit);
         a.ranges = ceil_div(n, a.rows);
-        if (p.cl <= 16 || (int64_t)a.tiles * a.ranges >= 256) break;
+        if (finish || p.cl <= 16 || (int64_t)a.tiles * a.ranges >= 256) break;
     }
     a.splits = 1;
     while (a.splits < 8 && (int64_t)a.ranges * a.tiles * a.splits < 512 && a.rows / (2 * a.splits) >= unit) a.splits *= 2;
     p.row_part = 16 * (size_t)a.ranges * (size_t)B;
     p.firsts = p.row_part + (a.tiles > 1 ? 16 * (size_t)a.tiles * (size_t)n : 0);
-    p.total = (p.firsts + 4 * (size_t)B + 255) & ~(size_t)255;
+    p.ready = 0;
+    p.total = p.firsts + 4 * (size_t)B;
+    if (finish) {
+        p.ready = (p.total + 15) & ~(size_t)15;
+        p.total = p.ready + 16 * (size_t)B;
+    }
+    p.total = (p.total + 255) & ~(size_t)255;
     return p;
 }
 static dim3 norm_grid(const NormArgs &a, int splits) { return dim3((unsigned)(a.tiles * splits * (a.ranges < 8 ? a.ranges : (a.ranges + 7) & ~7))); }
@@ -507,8 +590,10 @@ static int forward(const float *x, const float *gamma, const float *beta, double
 {
     double2 *part = (double2 *)work;
     float *firsts = (float *)((char *)work + pl.firsts);
-    const NormArgs &a = pl.a;
+    NormArgs a = pl.a;
+    a.ready = pl.ready ? (double2 *)((char *)work + pl.ready) : nullptr;
     hipLaunchKernelGGL((k_norm_sums<CL, SMALL, PAST>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
+    if (a.ready) hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part, firsts, eps, stats);
     hipLaunchKernelGGL((k_norm_apply<CL, SMALL, PAST>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts, y, stats);
     return sdnn_launched();
 }
@@ -538,22 +623,25 @@ template <int CL, bool SMALL, bool PAST, class Block>
 static int backward(const float *dy, const Block &x, const double *stats, const float *gamma, float *dx, RowSums rs, void *work, const NormPlan &pl, hipStream_t stream)
 {
     double2 *part = (double2 *)work;
-    const NormArgs &a = pl.a;
+    NormArgs a = pl.a;
+    a.ready = pl.ready ? (double2 *)((char *)work + pl.ready) : nullptr;
     rs.part = a.tiles > 1 ? (double *)((char *)work + pl.row_part) : nullptr;
     hipLaunchKernelGGL((k_norm_grad_sums<CL, SMALL, PAST, Block>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, rs);
+    if (dx && a.ready) hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part, (const float *)nullptr, 0.0, (double *)nullptr);
     if (dx || rs.part)
         hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, PAST, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, dx, rs);
     return sdnn_launched();
 }
-template <bool PACKED>
-static int backward_any(const float *dy, const float *x, const PackedBlock &x8, const double *stats, const float *gamma, int n, int B, float *dx, float *dgamma,
+// KIND 0: x; 1 and 2: x8, of values of both signs and of activations
+template <int KIND>
+static int backward_any(const float *dy, const float *x, const PackedArgs &x8, const double *stats, const float *gamma, int n, int B, float *dx, float *dgamma,
                         float *dbeta, void *work, void *stream_)
 {
     const NormPlan pl = plan_norm(n, B);
     const RowSums rs{nullptr, dgamma, dbeta};
     hipStream_t stream = (hipStream_t)stream_;
     auto go = [&](auto cl, auto small, auto past) {
-        if constexpr (PACKED) return backward<cl.value, small.value, past.value>(dy, x8, stats, gamma, dx, rs, work, pl, stream);
+        if constexpr (KIND > 0) return backward<cl.value, small.value, past.value>(dy, PackedBlock<KIND == 1>{x8}, stats, gamma, dx, rs, work, pl, stream);
         else return backward<cl.value, small.value, past.value>(dy, PlainBlock<past.value>{x}, stats, gamma, dx, rs, work, pl, stream);
     };
     const std::integral_constant<bool, true> yes;
@@ -582,7 +670,7 @@ extern "C" int sdnn_layernorm_backward(const float *d_dY, const float *d_X, cons
     if (!rc) rc = check_backward(d_dY, d_stats, d_dX, d_dgamma, d_dbeta);
     if (rc) return rc;
     if (!d_X) return sdnn_fail(SDNN_EINVAL, "d_X is NULL");
-    return backward_any<false>(d_dY, d_X, PackedBlock(), d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
+    return backward_any<0>(d_dY, d_X, PackedArgs(), d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
 }
 
 extern "C" int sdnn_layernorm_backward_packed(const float *d_dY, const void *d_packed, size_t packed_bytes, float cap, const double *d_stats,
@@ -593,9 +681,10 @@ extern "C" int sdnn_layernorm_backward_packed(const float *d_dY, const void *d_p
     if (!rc) rc = check_backward(d_dY, d_stats, d_dX, d_dgamma, d_dbeta);
     if (!rc) rc = sdnn_check_pack8(d_packed, packed_bytes, n, B, cap);
     if (rc) return rc;
-    PackedBlock x;
+    PackedArgs x;
     x.codes = (const uint8_t *)d_packed;
     x.scales = (const uint16_t *)(x.codes + PACK_GROUP * pack8_groups((int64_t)n * B));
     x.cap = cap; x.below = nextafterf(cap, 0.0f);
-    return backward_any<true>(d_dY, nullptr, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
+    return cap > 0.0f ? backward_any<2>(d_dY, nullptr, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream)
+                      : backward_any<1>(d_dY, nullptr, x, d_stats, d_gamma, n, B, d_dX, d_dgamma, d_dbeta, d_work, stream);
 }

@@ -47,13 +47,16 @@ __device__ __forceinline__ unsigned pack8_code(float x, float cap, double invers
     return live ? (unsigned)(x < 0.0f ? -c : c) & 255u : 128u;
 }
 // below: the largest float below cap
+template <bool SIGNED> __device__ __forceinline__ float pack8_value_of(unsigned code, float scale, float cap, float below)
+{
+    if constexpr (SIGNED) return code == 128u ? __builtin_nanf("") : (float)(int)(signed char)code * scale;
+    float v = fminf((float)code * scale, below);
+    v = code == 254u ? __builtin_nanf("") : v;
+    return code == 255u ? cap : v;
+}
 __device__ __forceinline__ float pack8_value(unsigned code, float scale, float cap, float below)
 {
-    if (cap > 0.0f) {
-        const float v = fminf((float)code * scale, below);
-        return code == 255u ? cap : code == 254u ? __builtin_nanf("") : v;
-    }
-    return code == 128u ? __builtin_nanf("") : (float)(int)(signed char)code * scale;
+    return cap > 0.0f ? pack8_value_of<false>(code, scale, cap, below) : pack8_value_of<true>(code, scale, cap, below);
 }
 
 // ---- host side, shared by the operators on single blocks ----------------------------------------------------------------
