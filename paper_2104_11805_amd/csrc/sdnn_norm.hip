@@ -36,7 +36,8 @@ template <int CL, bool SMALL> struct Columns {
     }
     __device__ __forceinline__ unsigned at() const { return (unsigned)(lane_row * B + base); } // from the start of the wavefront's first row
 
-    template <class T> __device__ __forceinline__ T *in(T *p) const { return (T *)((uintptr_t)p + 4u * at()); } // (32 bits beside a uniform address)
+    __device__ __forceinline__ const float *in(const float *p) const { return (const float *)((const char *)p + 4u * at()); } // 32 bits beside a uniform address
+    __device__ __forceinline__ float *in(float *p) const { return (float *)((char *)p + 4u * at()); }
     __device__ __forceinline__ bool any() const { return first < B; }
     __device__ __forceinline__ bool whole() const { return !SMALL && base == first; }
     __device__ __forceinline__ bool own(int v) const { return SMALL ? v < B : base + v >= first; }
@@ -137,6 +138,23 @@ __device__ __forceinline__ void store_column_sums(const C &c, const double (&a)[
     }
 }
 
+// The sums of every step-th range from k on, eight of them requested at a time; part: of a column.
+__device__ __forceinline__ double2 add_ranges(const double2 *__restrict__ part, int B, int k, int step, int ranges)
+{
+    double2 s = make_double2(0.0, 0.0);
+    for (; k < ranges; k += 8 * step) {
+        double2 t[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) t[u] = k + u * step < ranges ? part[(size_t)(k + u * step) * B] : make_double2(0.0, 0.0);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            s.x += t[u].x;
+            s.y += t[u].y;
+        }
+    }
+    return s;
+}
+
 // The sums of all ranges for the tile's columns, put through `finish`; the results for the lane's columns.  ready: there they are.
 template <int CL, class C, class F>
 __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__restrict__ part, int ranges, const double2 *__restrict__ ready, double (&a)[4],
@@ -149,13 +167,7 @@ __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__re
         if (tid < CT && col < c.B) lds[tid] = ready[col];
     } else {
         double2 s = make_double2(0.0, 0.0);
-        if (col < c.B)
-#pragma unroll 8
-            for (int k = tid / CT; k < ranges; k += K) {
-                const double2 t = part[(size_t)k * c.B + col];
-                s.x += t.x;
-                s.y += t.y;
-            }
+        if (col < c.B) s = add_ranges(part + col, c.B, tid / CT, K, ranges);
         lds[tid] = s;
         __syncthreads();
         if (tid < CT) {
@@ -181,6 +193,13 @@ __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__re
 template <int CL> __device__ __forceinline__ int first_row(int r0) { return r0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * (64 / CL); }
 template <int CL> __device__ __forceinline__ int row_of(int r, int u) { return r + u * (NORM_THREADS / CL); }
 template <int CL> __device__ __forceinline__ int next_rows(int r) { return row_of<CL>(r, NORM_ROWS); }
+// Whether all of them are there.  Then nothing is asked row by row: a condition around a row's loads has the compiler move what is done with
+// them to where they are, and a row waits for the one before it.  Lanes without columns of their own read their neighbours'.
+template <int CL> __device__ __forceinline__ bool full_rows(int r, int r1) { return row_of<CL>(r, NORM_ROWS - 1) + 64 / CL <= r1; }
+typedef std::integral_constant<bool, true> Full;
+typedef std::integral_constant<bool, false> Rest;
+// gamma or beta of a row: `other`, which has n values and more, is read where there is none, and dropped where the value is used
+__device__ __forceinline__ float of_row(const float *p, const float *other, int row) { return (p ? p : other)[row]; }
 template <class C> __device__ __forceinline__ size_t first_start(const C &c, int r) { return (size_t)r * (size_t)c.B; }
 template <int CL, class C> __device__ __forceinline__ size_t start_of(const C &c, size_t e, int u) { return e + (size_t)u * (NORM_THREADS / CL) * (size_t)c.B; }
 template <int CL, class C> __device__ __forceinline__ size_t next_start(const C &c, size_t e) { return start_of<CL>(c, e, NORM_ROWS); }
@@ -205,13 +224,7 @@ __global__ void __launch_bounds__(512) k_norm_finish(const NormArgs a, const dou
     __shared__ double2 lds[512];
     const int tid = threadIdx.x, col = (int)blockIdx.x * FINISH_COLUMNS + (tid & (FINISH_COLUMNS - 1));
     double2 s = make_double2(0.0, 0.0);
-    if (col < a.B)
-#pragma unroll 8
-        for (int k = tid / FINISH_COLUMNS; k < a.ranges; k += 512 / FINISH_COLUMNS) {
-            const double2 t = part[(size_t)k * a.B + col];
-            s.x += t.x;
-            s.y += t.y;
-        }
+    if (col < a.B) s = add_ranges(part + col, a.B, tid / FINISH_COLUMNS, 512 / FINISH_COLUMNS, a.ranges);
     lds[tid] = s;
     __syncthreads();
     if (tid >= FINISH_COLUMNS || col >= a.B) return;
@@ -258,36 +271,40 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restr
     const Columns<CL, SMALL> c(tile, a.B);
     const PlainBlock<PAST> in{x};
     double s1[4] = {}, s2[4] = {};
-    if (c.any()) {
-        typename PlainBlock<PAST>::Raw first, t[NORM_ROWS];
+    float first[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) first.v[v] = x[min(c.base + v, a.B - 1)];
-        if (range == 0 && (int)threadIdx.x < CL)
+    for (int v = 0; v < 4; ++v) first[v] = x[min(c.base + v, a.B - 1)];
+    if (range == 0 && (int)threadIdx.x < CL && c.any())
 #pragma unroll
-            for (int v = 0; v < 4; ++v)
-                if (c.own(v)) firsts[c.base + v] = first.v[v];
-        size_t e = first_start(c, first_row<CL>(r0));
-        for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r), e = next_start<CL>(c, e)) {
+        for (int v = 0; v < 4; ++v)
+            if (c.own(v)) firsts[c.base + v] = first[v];
+    int r = first_row<CL>(r0);
+    size_t e = first_start(c, r);
+    auto rows = [&](auto full) {
+        typename PlainBlock<PAST>::Raw t[NORM_ROWS];
 #pragma unroll
-            for (int u = 0; u < NORM_ROWS; ++u)
-                if (row_of<CL>(r, u) + c.lane_row < r1) in.request(c, start_of<CL>(c, e, u), t[u]);
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) in.request(c, start_of<CL>(c, e, u), t[u]);
 #pragma unroll
-            for (int u = 0; u < NORM_ROWS; ++u)
-                if (row_of<CL>(r, u) + c.lane_row < r1)
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1)
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const double d = (double)t[u].v[v] - (double)first.v[v];
-                        s1[v] += d;
-                        s2[v] = fma(d, d, s2[v]);
-                    }
-        }
-    }
+                for (int v = 0; v < 4; ++v) {
+                    const double d = (double)t[u].v[v] - (double)first[v];
+                    s1[v] += d;
+                    s2[v] = fma(d, d, s2[v]);
+                }
+        r = next_rows<CL>(r);
+        e = next_start<CL>(c, e);
+    };
+    while (full_rows<CL>(r, r1)) rows(Full());
+    while (r < r1) rows(Rest());
     store_column_sums<CL>(c, s1, s2, part + (size_t)range * a.B);
 }
 
 template <class C> __device__ __forceinline__ void store_row(const C &c, float *p, const float (&o)[4])
 {
-    if (c.whole()) {
+    if (c.whole()) { // (not so for lanes without columns)
         __builtin_nontemporal_store(F4{o[0], o[1], o[2], o[3]}, reinterpret_cast<F4 *>(p));
     } else {
 #pragma unroll
@@ -305,22 +322,20 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
     if (!find_tile(a, a.splits, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
     const PlainBlock<PAST> in{x};
-    struct Rows {
-        typename PlainBlock<PAST>::Raw t[NORM_ROWS];
-        float g[NORM_ROWS], b[NORM_ROWS];
-    } now;
-    auto request = [&](int r, size_t e, Rows &w) {
-#pragma unroll
-        for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) + c.lane_row < r1 && c.any()) {
-                in.request(c, start_of<CL>(c, e, u), w.t[u]);
-                w.g[u] = gamma ? gamma[row_of<CL>(r, u) + c.lane_row] : 1.0f;
-                w.b[u] = beta ? beta[row_of<CL>(r, u) + c.lane_row] : 0.0f;
-            }
-    };
     int r = first_row<CL>(r0);
     size_t e = first_start(c, r);
-    request(r, e, now); // on their way while the sums are added up
+    typename PlainBlock<PAST>::Raw t[NORM_ROWS];
+    float g[NORM_ROWS], b[NORM_ROWS];
+    auto request = [&](auto full) {
+#pragma unroll
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
+                in.request(c, start_of<CL>(c, e, u), t[u]);
+                g[u] = of_row(gamma, x, row_of<CL>(r, u) + c.lane_row);
+                b[u] = of_row(beta, x, row_of<CL>(r, u) + c.lane_row);
+            }
+    };
+    if (full_rows<CL>(r, r1)) request(Full()); // on their way while the sums are added up
     double mean[4], rstd[4];
     const double inv = 1.0 / (double)a.n;
     load_column_sums<CL>(c, part, a.ranges, a.ready, mean, rstd, [&](int col, double2 s) {
@@ -331,19 +346,116 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
         }
         return out;
     });
-    if (!c.any()) return;
     double shift[4]; // h = (x - mean) rstd as x rstd + shift
 #pragma unroll
     for (int v = 0; v < 4; ++v) shift[v] = -mean[v] * rstd[v];
-    for (; r < r1; r = next_rows<CL>(r), e = next_start<CL>(c, e), request(r, e, now)) {
+    auto rows = [&](auto full) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) + c.lane_row < r1) {
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
+                const double gd = gamma ? (double)g[u] : 1.0, bd = beta ? (double)b[u] : 0.0;
                 float o[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)now.t[u].v[v], rstd[v], shift[v]), (double)now.g[u], (double)now.b[u]);
+                for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)t[u].v[v], rstd[v], shift[v]), gd, bd);
                 store_row(c, c.in(y + start_of<CL>(c, e, u)), o);
             }
+        r = next_rows<CL>(r);
+        e = next_start<CL>(c, e);
+    };
+    while (full_rows<CL>(r, r1)) {
+        rows(Full());
+        if (full_rows<CL>(r, r1)) request(Full());
+    }
+    while (r < r1) {
+        request(Rest());
+        rows(Rest());
+    }
+}
+
+// Blocks of so few rows that a workgroup holds all of them of CL * 4 columns in registers, ROWS per thread: one launch, and every value is read
+// once.
+#define WHOLE_THREADS 1024
+template <int CL, int ROWS, bool PAST>
+__global__ void __launch_bounds__(WHOLE_THREADS) k_norm_whole(const float *x, const float *__restrict__ gamma, const float *__restrict__ beta, int n, int B, double eps,
+                                                              double inv, float *y, double *__restrict__ stats)
+{
+    constexpr int CT = 4 * CL, WAVES = WHOLE_THREADS / 64, STEP = WHOLE_THREADS / CL;
+    __shared__ double2 lds[WAVES][CT];
+    // an XCD takes neighbouring columns: they share cache lines
+    const int per = (int)gridDim.x >> 3, id = (int)blockIdx.x, tid = threadIdx.x;
+    const Columns<CL, false> c(id < 8 * per ? (id & 7) * per + (id >> 3) : id, B);
+    const int r = __builtin_amdgcn_readfirstlane(tid >> 6) * (64 / CL);
+    // all that is read is requested before anything waits for it
+    const int lane_first = c.tile0 + (tid & ~3), col = min(lane_first, B - 4) + (tid & 3); // of the statistics that this thread makes
+    typename PlainBlock<PAST>::Raw t[ROWS];
+    float first[4], g[ROWS], b[ROWS], own_first = 0.0f;
+    if (tid < CT && lane_first < B) own_first = x[col];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) first[v] = x[c.base + v];
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) { // (rows that are not there: the last one again)
+        const int row = min(r + u * STEP + c.lane_row, n - 1);
+        const F4 f = PAST ? __builtin_nontemporal_load(reinterpret_cast<const F4 *>(x + (size_t)row * (size_t)B + (size_t)c.base))
+                          : *reinterpret_cast<const F4 *>(x + (size_t)row * (size_t)B + (size_t)c.base);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) t[u].v[v] = f[v];
+        g[u] = of_row(gamma, x, row);
+        b[u] = of_row(beta, x, row);
+    }
+    double s1[4] = {}, s2[4] = {};
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u)
+            if (r + u * STEP + c.lane_row < n) {
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const double d = (double)t[u].v[v] - (double)first[v];
+                    s1[v] += d;
+                    s2[v] = fma(d, d, s2[v]);
+                }
+                // added here: else the rows' values are converted ahead, which takes twice their registers
+                asm volatile("" : "+v"(s1[0]), "+v"(s1[1]), "+v"(s1[2]), "+v"(s1[3]), "+v"(s2[0]), "+v"(s2[1]), "+v"(s2[2]), "+v"(s2[3]));
+            }
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const double2 s = make_double2(add_rows<CL>(s1[v]), add_rows<CL>(s2[v]));
+        if ((tid & 63) < CL) lds[tid >> 6][4 * (tid & 63) + v] = s;
+    }
+    __syncthreads();
+    if (tid < CT) {
+        double2 s = lds[0][tid];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            s.x += lds[w][tid].x;
+            s.y += lds[w][tid].y;
+        }
+        if (lane_first < B) {
+            s = statistics(s, own_first, inv, eps);
+            if (stats && col >= lane_first) {
+                stats[col] = s.x;
+                stats[B + col] = s.y;
+            }
+            lds[0][tid] = s;
+        }
+    }
+    __syncthreads(); // (and y may be x: everyone has read all that it needs of it)
+    if (!c.any()) return;
+    double rstd[4], shift[4];
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const double2 s = lds[0][4 * (tid & (CL - 1)) + v];
+        rstd[v] = s.y;
+        shift[v] = -s.x * s.y;
+    }
+#pragma unroll
+    for (int u = 0; u < ROWS; ++u) {
+        const int row = r + u * STEP + c.lane_row;
+        if (row < n) {
+            const double gd = gamma ? (double)g[u] : 1.0, bd = beta ? (double)b[u] : 0.0;
+            float o[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)t[u].v[v], rstd[v], shift[v]), gd, bd);
+            store_row(c, y + (size_t)row * (size_t)B + (size_t)c.base, o);
+        }
     }
 }
 
@@ -394,27 +506,30 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float 
     const PlainBlock<PAST> up{dy};
     double p[4] = {}, q[4] = {}, shift[4] = {}, rstd[4] = {}; // h = (x - mean) rstd as x rstd + shift
 #pragma unroll
-    for (int v = 0; v < 4; ++v)
-        if (c.any() && c.own(v)) {
-            rstd[v] = stats[a.B + c.base + v];
-            shift[v] = -stats[c.base + v] * rstd[v];
-        }
-    size_t e = first_start(c, first_row<CL>(r0));
-    for (int r = first_row<CL>(r0); r < r1; r = next_rows<CL>(r), e = next_start<CL>(c, e)) {
+    for (int v = 0; v < 4; ++v) {
+        const int col = min(c.base + v, a.B - 1);
+        const double mean = stats[col], k = stats[a.B + col];
+        rstd[v] = c.own(v) ? k : 0.0; // (columns that are not the lane's own must add nothing to the rows' sums)
+        shift[v] = c.own(v) ? -mean * k : 0.0;
+    }
+    int r = first_row<CL>(r0);
+    size_t e = first_start(c, r);
+    auto rows = [&](auto full) {
         typename PlainBlock<PAST>::Raw d[NORM_ROWS];
         typename Block::Raw t[NORM_ROWS];
         float g[NORM_ROWS];
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) + c.lane_row < r1 && c.any()) {
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
                 up.request(c, start_of<CL>(c, e, u), d[u]);
                 x.request(c, start_of<CL>(c, e, u), t[u]);
-                g[u] = gamma ? gamma[row_of<CL>(r, u) + c.lane_row] : 1.0f;
+                g[u] = of_row(gamma, dy, row_of<CL>(r, u) + c.lane_row);
             }
         double sum[8] = {};
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) + c.lane_row < r1 && c.any()) {
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
+                const double gr = gamma ? (double)g[u] : 1.0;
                 float xv[4];
                 x.values(c, t[u], xv);
                 if (c.ragged())
@@ -423,7 +538,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float 
                         if (!c.own(v)) d[u].v[v] = xv[v] = 0.0f;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const double h = fma((double)xv[v], rstd[v], shift[v]), dv = (double)d[u].v[v], gd = (double)g[u] * dv;
+                    const double h = fma((double)xv[v], rstd[v], shift[v]), dv = (double)d[u].v[v], gd = gr * dv;
                     p[v] += gd;
                     q[v] = fma(gd, h, q[v]);
                     sum[2 * u] = fma(dv, h, sum[2 * u]);
@@ -437,14 +552,18 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float 
 #pragma unroll
             for (int j = 0; j < n_sums; ++j) {
                 const int u = (first + j) >> 1, w = (first + j) & 1;
-                const size_t row = (size_t)(row_of<CL>(r, u) + c.lane_row);
-                if (row < (size_t)r1) {
+                const int row = row_of<CL>(r, u) + c.lane_row;
+                if (full.value || row < r1) {
                     if (rs.part) rs.part[2 * ((size_t)tile * a.n + row) + w] = sum[j];
                     else if (w == 0 && rs.dgamma) rs.dgamma[row] = (float)sum[j];
                     else if (w == 1 && rs.dbeta) rs.dbeta[row] = (float)sum[j];
                 }
             }
-    }
+        r = next_rows<CL>(r);
+        e = next_start<CL>(c, e);
+    };
+    while (full_rows<CL>(r, r1)) rows(Full());
+    while (r < r1) rows(Rest());
     store_column_sums<CL>(c, p, q, part + (size_t)range * a.B);
 }
 
@@ -459,8 +578,12 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float
         const int share = (r1 - r0 + a.tiles - 1) / a.tiles, end = 2 * min(r1, r0 + (tile + 1) * share);
         for (int i = 2 * (r0 + tile * share) + (int)threadIdx.x; i < end; i += NORM_THREADS) {
             double s = 0.0;
-#pragma unroll 4
-            for (int k = 0; k < a.tiles; ++k) s += rs.part[2 * (size_t)k * a.n + i];
+            for (int k = 0; k < a.tiles; k += 4) {
+                double t[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) t[u] = k + u < a.tiles ? rs.part[2 * (size_t)(k + u) * a.n + i] : 0.0;
+                s += (t[0] + t[1]) + (t[2] + t[3]);
+            }
             float *out = i & 1 ? rs.dbeta : rs.dgamma;
             if (out) out[i >> 1] = (float)s;
         }
@@ -468,46 +591,59 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float
     if (!dx) return;
     const Columns<CL, SMALL> c(tile, a.B);
     const PlainBlock<PAST> up{dy};
-    struct Rows {
-        typename PlainBlock<PAST>::Raw d[NORM_ROWS];
-        typename Block::Raw t[NORM_ROWS];
-        float g[NORM_ROWS];
-    } now;
-    auto request = [&](int r, size_t e, Rows &w) {
-#pragma unroll
-        for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) + c.lane_row < r1 && c.any()) {
-                up.request(c, start_of<CL>(c, e, u), w.d[u]);
-                x.request(c, start_of<CL>(c, e, u), w.t[u]);
-                w.g[u] = gamma ? gamma[row_of<CL>(r, u) + c.lane_row] : 1.0f;
-            }
-    };
     int r = first_row<CL>(r0);
     size_t e = first_start(c, r);
-    request(r, e, now); // on their way while the sums are added up
-    double p[4], q[4], rstd[4] = {}; // dX = (g rstd) dY - p - q x: p and q become those constants of a column
-    const double inv = 1.0 / (double)a.n;
-    load_column_sums<CL>(c, part, a.ranges, a.ready, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
-    if (!c.any()) return;
-#pragma unroll
-    for (int v = 0; v < 4; ++v)
-        if (c.own(v)) {
-            const double r = stats[a.B + c.base + v], t = r * q[v];
-            rstd[v] = r;
-            p[v] = fma(-stats[c.base + v] * r, t, r * p[v]);
-            q[v] = r * t;
-        }
-    for (; r < r1; r = next_rows<CL>(r), e = next_start<CL>(c, e), request(r, e, now)) {
+    typename PlainBlock<PAST>::Raw d[NORM_ROWS];
+    typename Block::Raw t[NORM_ROWS];
+    float g[NORM_ROWS];
+    auto request = [&](auto full) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (row_of<CL>(r, u) + c.lane_row < r1) {
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
+                up.request(c, start_of<CL>(c, e, u), d[u]);
+                x.request(c, start_of<CL>(c, e, u), t[u]);
+                g[u] = of_row(gamma, dy, row_of<CL>(r, u) + c.lane_row);
+            }
+    };
+    double mean[4] = {}, rstd[4] = {};
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const int col = min(c.base + v, a.B - 1);
+        mean[v] = stats[col];
+        rstd[v] = stats[a.B + col];
+    }
+    if (full_rows<CL>(r, r1)) request(Full()); // on their way while the sums are added up
+    double p[4], q[4]; // dX = (g rstd) dY - p - q x: p and q become those constants of a column
+    const double inv = 1.0 / (double)a.n;
+    load_column_sums<CL>(c, part, a.ranges, a.ready, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+        const double k = rstd[v] * q[v];
+        p[v] = fma(-mean[v] * rstd[v], k, rstd[v] * p[v]);
+        q[v] = rstd[v] * k;
+    }
+    auto rows = [&](auto full) {
+#pragma unroll
+        for (int u = 0; u < NORM_ROWS; ++u)
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
+                const double gr = gamma ? (double)g[u] : 1.0;
                 float xv[4], o[4];
-                x.values(c, now.t[u], xv);
+                x.values(c, t[u], xv);
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    o[v] = (float)fma((double)now.g[u] * rstd[v], (double)now.d[u].v[v], -fma(q[v], (double)xv[v], p[v]));
+                    o[v] = (float)fma(gr * rstd[v], (double)d[u].v[v], -fma(q[v], (double)xv[v], p[v]));
                 store_row(c, c.in(dx + start_of<CL>(c, e, u)), o);
             }
+        r = next_rows<CL>(r);
+        e = next_start<CL>(c, e);
+    };
+    while (full_rows<CL>(r, r1)) {
+        rows(Full());
+        if (full_rows<CL>(r, r1)) request(Full());
+    }
+    while (r < r1) {
+        request(Rest());
+        rows(Rest());
     }
 }
 
@@ -516,6 +652,7 @@ static int across(int B) { return B < 4 ? 1 : B <= 16 ? 4 : B <= 32 ? 8 : B <= 6
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Tiles: enough workgroups to fill the chip, but not so many ranges that their sums are a load to add up.
+#define PAST_COUNT ((int64_t)48 << 20) // blocks of 200 MB and more are read past the caches
 // From so many values on, the ranges' sums are added up by a launch of their own (4 us); below, every workgroup of the second launch does
 // so for its columns, of fewer ranges.
 #ifndef FINISH_COUNT
@@ -532,7 +669,7 @@ static NormPlan plan_norm(int n, int B)
     NormPlan p;
     NormArgs &a = p.a;
     a.n = n; a.B = B;
-    p.past = (int64_t)n * B >= (int64_t)48 << 20;
+    p.past = (int64_t)n * B >= PAST_COUNT;
     const bool finish = (int64_t)n * B >= FINISH_COUNT;
     int unit;
     for (p.cl = across(B);; p.cl /= 2) {
@@ -545,7 +682,7 @@ static NormPlan plan_norm(int n, int B)
         if (finish || p.cl <= 16 || (int64_t)a.tiles * a.ranges >= 256) break;
     }
     a.splits = 1;
-    while (a.splits < 8 && (int64_t)a.ranges * a.tiles * a.splits < 512 && a.rows / (2 * a.splits) >= unit) a.splits *= 2;
+    while (a.splits < 8 && (int64_t)a.ranges * a.tiles * a.splits < 512 && a.rows % (2 * a.splits * unit) == 0) a.splits *= 2;
     p.row_part = 16 * (size_t)a.ranges * (size_t)B;
     p.firsts = p.row_part + (a.tiles > 1 ? 16 * (size_t)a.tiles * (size_t)n : 0);
     p.ready = 0;
@@ -585,6 +722,21 @@ extern "C" int sdnn_layernorm_workspace_bytes(int32_t n, int32_t B, size_t *byte
     return SDNN_OK;
 }
 
+// Whether a block takes k_norm_whole: lanes across, or 0.
+static int whole_lanes(int n, int B)
+{
+    if (B < 4 || n > 4096) return 0;
+    return n > 2048 ? ((int64_t)n * B <= 3 << 20 ? 2 : 0) : n <= 1024 && B >= 4096 ? 8 : 4;
+}
+template <int CL, int ROWS>
+static int forward_whole(const float *x, const float *gamma, const float *beta, int n, int B, double eps, float *y, double *stats, hipStream_t stream)
+{
+    const dim3 grid((unsigned)ceil_div(B, 4 * CL)), block(WHOLE_THREADS);
+    if (CL > 2 && ROWS > 4 && (int64_t)n * B >= PAST_COUNT)
+        hipLaunchKernelGGL((k_norm_whole<CL, ROWS, (CL > 2 && ROWS > 4)>), grid, block, 0, stream, x, gamma, beta, n, B, eps, 1.0 / (double)n, y, stats);
+    else hipLaunchKernelGGL((k_norm_whole<CL, ROWS, false>), grid, block, 0, stream, x, gamma, beta, n, B, eps, 1.0 / (double)n, y, stats);
+    return sdnn_launched();
+}
 template <int CL, bool SMALL, bool PAST>
 static int forward(const float *x, const float *gamma, const float *beta, double eps, float *y, double *stats, void *work, const NormPlan &pl, hipStream_t stream)
 {
@@ -607,6 +759,13 @@ extern "C" int sdnn_layernorm(const float *d_X, const float *d_gamma, const floa
     if (!(eps > 0.0) || !(eps <= 1e30)) return sdnn_fail(SDNN_EINVAL, "eps must be > 0");
     const NormPlan pl = plan_norm(n, B);
     hipStream_t stream = (hipStream_t)stream_;
+    switch (whole_lanes(n, B)) {
+    case 2: return forward_whole<2, 8>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, stream);
+    case 4:
+        return n <= 1024 ? forward_whole<4, 4>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, stream)
+                         : forward_whole<4, 8>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, stream);
+    case 8: return forward_whole<8, 8>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, stream);
+    }
     switch (pl.cl) {
     case 1: return forward<1, true, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
     case 4: return forward<4, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);

@@ -165,7 +165,7 @@ def sdnn_deal_rows_to_xcds(n_rows, row_ptr, order):
 def _stream_ptr(stream=None):
     import torch
     if stream is None:  # the current one, without making an object of it (2.7 us)
-        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+        return C.c_void_p(_raw_stream())
     return C.c_void_p(stream.cuda_stream)
 
 
@@ -382,6 +382,15 @@ def sdnn_gather_probe(table, v: int, idx_i32, n_waves: int, per_wave: int, out, 
 
 # ---- blocks: activations in 8 bits, layer norm -------------------------------------
 
+def _raw_stream() -> int:
+    import torch
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
 def sdnn_pack8_bytes(n: int, b: int) -> int:
     nbytes = C.c_size_t(0)
     _check(lib().sdnn_pack8_bytes(int(n), int(b), C.byref(nbytes)))
@@ -404,7 +413,7 @@ def sdnn_pack8(x, cap: float = 0.0, packed=None, stream=None) -> Packed8:
             return sdnn_pack8(x, cap, packed)
     if packed is None:
         packed = torch.empty(sdnn_pack8_bytes(n, b), dtype=torch.uint8, device=x.device)
-    _check(lib().sdnn_pack8(_dp(x), n, b, cap, _dp(_bytes(packed, "packed", index)), packed.numel(), _stream_ptr()))
+    _check(lib().sdnn_pack8(x.data_ptr(), n, b, cap, _bytes(packed, "packed", index).data_ptr(), packed.numel(), _raw_stream()))
     return Packed8(packed, n, b, cap)
 
 
@@ -417,7 +426,7 @@ def sdnn_unpack8(packed: Packed8, x=None, stream=None):
     if x is None:
         x = torch.empty(packed.n, packed.b, device=packed.data.device)
     _tensor(x, "x", (packed.n, packed.b), torch.float32, index)
-    _check(lib().sdnn_unpack8(_dp(packed.data), packed.data.numel(), packed.n, packed.b, packed.cap, _dp(x), _stream_ptr()))
+    _check(lib().sdnn_unpack8(packed.data.data_ptr(), packed.data.numel(), packed.n, packed.b, packed.cap, x.data_ptr(), _raw_stream()))
     return x
 
 
@@ -448,7 +457,7 @@ def sdnn_layernorm(x, gamma=None, beta=None, eps: float = 1e-5, y=None, stats=No
     work = _work(work, n, b, index)
     y = torch.empty_like(x) if y is None else _tensor(y, "y", (n, b), torch.float32, index)
     stats = torch.empty((2, b), dtype=torch.float64, device=x.device) if stats is None else _tensor(stats, "stats", (2, b), torch.float64, index)
-    _check(lib().sdnn_layernorm(_dp(x), _dp(gamma), _dp(beta), n, b, eps, _dp(y), _dp(stats), _dp(work), work.numel(), _stream_ptr()))
+    _check(lib().sdnn_layernorm(x.data_ptr(), _ptr(gamma), _ptr(beta), n, b, eps, y.data_ptr(), stats.data_ptr(), work.data_ptr(), work.numel(), _raw_stream()))
     return y, stats
 
 
@@ -473,9 +482,9 @@ def sdnn_layernorm_backward(dy, x, stats, gamma=None, dx=None, dgamma=None, dbet
     dx = torch.empty_like(dy) if dx is None else _tensor(dx, "dx", (n, b), torch.float32, index)
     dgamma = dy.new_empty(n) if dgamma is None else _tensor(dgamma, "dgamma", (n,), torch.float32, index)
     dbeta = dy.new_empty(n) if dbeta is None else _tensor(dbeta, "dbeta", (n,), torch.float32, index)
-    out = (n, b, _dp(dx), _dp(dgamma), _dp(dbeta), _dp(work), work.numel(), _stream_ptr())
+    out = (n, b, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), work.data_ptr(), work.numel(), _raw_stream())
     if packed:
-        _check(lib().sdnn_layernorm_backward_packed(_dp(dy), _dp(x.data), x.data.numel(), x.cap, _dp(stats), _dp(gamma), *out))
+        _check(lib().sdnn_layernorm_backward_packed(dy.data_ptr(), x.data.data_ptr(), x.data.numel(), x.cap, stats.data_ptr(), _ptr(gamma), *out))
     else:
-        _check(lib().sdnn_layernorm_backward(_dp(dy), _dp(x), _dp(stats), _dp(gamma), *out))
+        _check(lib().sdnn_layernorm_backward(dy.data_ptr(), x.data_ptr(), stats.data_ptr(), _ptr(gamma), *out))
     return dx, dgamma, dbeta
