@@ -16,20 +16,22 @@
 
 #define NORM_THREADS 512
 #define NORM_ROWS 4
+#define BESIDE 4 // wavefronts that lie beside each other in a second launch over wide rows
 
 typedef float F4 __attribute__((ext_vector_type(4), aligned(4))); // 16 bytes at any multiple of 4
 struct __attribute__((packed, aligned(1))) U1 { unsigned v; }; // 4 bytes anywhere
 
+// BESIDE wavefronts may lie beside each other (CL = 64), each with a tile of its own.
 // A lane's four columns.  They end with the block's last column at the latest: the last lane's first ones may be its neighbour's, and
 // are left out of everything.  SMALL: B < 4, one lane across.
-template <int CL, bool SMALL> struct Columns {
+template <int CL, bool SMALL, int WX = 1> struct Columns {
     static constexpr bool small = SMALL;
     int tile0, B, lane_row;    // lane_row: of the rows that the wavefront has at a time
     int base, first;           // columns base .. base + 3, of which those from `first` on are the lane's own; none if first >= B
     __device__ __forceinline__ Columns(int tile, int B_)
     {
         B = B_;
-        tile0 = tile * 4 * CL;
+        tile0 = (tile * WX + (WX > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % WX : 0)) * 4 * CL;
         first = tile0 + 4 * (int)(threadIdx.x & (CL - 1));
         base = SMALL ? 0 : min(first, B - 4);
         lane_row = (int)(threadIdx.x & 63) / CL;
@@ -156,15 +158,20 @@ __device__ __forceinline__ double2 add_ranges(const double2 *__restrict__ part, 
 }
 
 // The sums of all ranges for the tile's columns, put through `finish`; the results for the lane's columns.  ready: there they are.
-template <int CL, class C, class F>
+template <int CL, bool READY, class C, class F>
 __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__restrict__ part, int ranges, const double2 *__restrict__ ready, double (&a)[4],
                                                  double (&b)[4], F finish)
 {
     constexpr int CT = 4 * CL, K = NORM_THREADS / CT;
     __shared__ double2 lds[NORM_THREADS];
     const int tid = threadIdx.x, col = c.tile0 + (tid & (CT - 1));
-    if (ready) {
-        if (tid < CT && col < c.B) lds[tid] = ready[col];
+    if constexpr (READY) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const double2 t = ready[min(c.base + v, c.B - 1)];
+            a[v] = t.x;
+            b[v] = t.y;
+        }
     } else {
         double2 s = make_double2(0.0, 0.0);
         if (col < c.B) s = add_ranges(part + col, c.B, tid / CT, K, ranges);
@@ -178,31 +185,31 @@ __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__re
             if (col < c.B) s = finish(col, s);
             lds[tid] = s;
         }
-    }
-    __syncthreads();
+        __syncthreads();
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const double2 t = lds[max(0, min(c.base + v - c.tile0, CT - 1))];
-        a[v] = t.x;
-        b[v] = t.y;
+        for (int v = 0; v < 4; ++v) {
+            const double2 t = lds[max(0, min(c.base + v - c.tile0, CT - 1))];
+            a[v] = t.x;
+            b[v] = t.y;
+        }
     }
 }
 
 // The rows that a wavefront walks: from its first one on 64 / CL at a time, the lane's is lane_row further, and NORM_ROWS times that, row_of<CL>(r,
 // u), are requested together.  r and where that row starts, e, are the same for the wavefront.
-template <int CL> __device__ __forceinline__ int first_row(int r0) { return r0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * (64 / CL); }
-template <int CL> __device__ __forceinline__ int row_of(int r, int u) { return r + u * (NORM_THREADS / CL); }
-template <int CL> __device__ __forceinline__ int next_rows(int r) { return row_of<CL>(r, NORM_ROWS); }
+template <int CL, int WX = 1> __device__ __forceinline__ int first_row(int r0) { return r0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / WX * (64 / CL); }
+template <int CL, int WX = 1> __device__ __forceinline__ int row_of(int r, int u) { return r + u * (NORM_THREADS / CL / WX); }
+template <int CL, int WX = 1> __device__ __forceinline__ int next_rows(int r) { return row_of<CL, WX>(r, NORM_ROWS); }
 // Whether all of them are there.  Then nothing is asked row by row: a condition around a row's loads has the compiler move what is done with
 // them to where they are, and a row waits for the one before it.  Lanes without columns of their own read their neighbours'.
-template <int CL> __device__ __forceinline__ bool full_rows(int r, int r1) { return row_of<CL>(r, NORM_ROWS - 1) + 64 / CL <= r1; }
+template <int CL, int WX = 1> __device__ __forceinline__ bool full_rows(int r, int r1) { return row_of<CL, WX>(r, NORM_ROWS - 1) + 64 / CL <= r1; }
 typedef std::integral_constant<bool, true> Full;
 typedef std::integral_constant<bool, false> Rest;
 // gamma or beta of a row: `other`, which has n values and more, is read where there is none, and dropped where the value is used
 __device__ __forceinline__ float of_row(const float *p, const float *other, int row) { return (p ? p : other)[row]; }
 template <class C> __device__ __forceinline__ size_t first_start(const C &c, int r) { return (size_t)r * (size_t)c.B; }
-template <int CL, class C> __device__ __forceinline__ size_t start_of(const C &c, size_t e, int u) { return e + (size_t)u * (NORM_THREADS / CL) * (size_t)c.B; }
-template <int CL, class C> __device__ __forceinline__ size_t next_start(const C &c, size_t e) { return start_of<CL>(c, e, NORM_ROWS); }
+template <int CL, int WX = 1, class C> __device__ __forceinline__ size_t start_of(const C &c, size_t e, int u) { return e + (size_t)u * (NORM_THREADS / CL / WX) * (size_t)c.B; }
+template <int CL, int WX = 1, class C> __device__ __forceinline__ size_t next_start(const C &c, size_t e) { return start_of<CL, WX>(c, e, NORM_ROWS); }
 
 struct NormArgs {
     int32_t n, B, rows;            // rows of a range
@@ -313,32 +320,32 @@ template <class C> __device__ __forceinline__ void store_row(const C &c, float *
     }
 }
 
-template <int CL, bool SMALL, bool PAST>
+template <int CL, bool SMALL, bool PAST, bool READY, int WX>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, const float *__restrict__ gamma, const float *__restrict__ beta, const NormArgs a,
                                                              double eps, const double2 *__restrict__ part, const float *__restrict__ firsts, float *y,
                                                              double *__restrict__ stats)
 {
     int tile, range, r0, r1;
     if (!find_tile(a, a.splits, tile, range, r0, r1)) return;
-    const Columns<CL, SMALL> c(tile, a.B);
+    const Columns<CL, SMALL, WX> c(tile, a.B);
     const PlainBlock<PAST> in{x};
-    int r = first_row<CL>(r0);
+    int r = first_row<CL, WX>(r0);
     size_t e = first_start(c, r);
     typename PlainBlock<PAST>::Raw t[NORM_ROWS];
     float g[NORM_ROWS], b[NORM_ROWS];
     auto request = [&](auto full) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
-                in.request(c, start_of<CL>(c, e, u), t[u]);
-                g[u] = of_row(gamma, x, row_of<CL>(r, u) + c.lane_row);
-                b[u] = of_row(beta, x, row_of<CL>(r, u) + c.lane_row);
+            if (full.value || row_of<CL, WX>(r, u) + c.lane_row < r1) {
+                in.request(c, start_of<CL, WX>(c, e, u), t[u]);
+                g[u] = of_row(gamma, x, row_of<CL, WX>(r, u) + c.lane_row);
+                b[u] = of_row(beta, x, row_of<CL, WX>(r, u) + c.lane_row);
             }
     };
-    if (full_rows<CL>(r, r1)) request(Full()); // on their way while the sums are added up
+    if (full_rows<CL, WX>(r, r1)) request(Full()); // on their way while the sums are added up
     double mean[4], rstd[4];
     const double inv = 1.0 / (double)a.n;
-    load_column_sums<CL>(c, part, a.ranges, a.ready, mean, rstd, [&](int col, double2 s) {
+    load_column_sums<CL, READY>(c, part, a.ranges, a.ready, mean, rstd, [&](int col, double2 s) {
         const double2 out = statistics(s, firsts[col], inv, eps);
         if (r0 == 0 && stats) {
             stats[col] = out.x;
@@ -352,19 +359,19 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
     auto rows = [&](auto full) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
+            if (full.value || row_of<CL, WX>(r, u) + c.lane_row < r1) {
                 const double gd = gamma ? (double)g[u] : 1.0, bd = beta ? (double)b[u] : 0.0;
                 float o[4];
 #pragma unroll
                 for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)t[u].v[v], rstd[v], shift[v]), gd, bd);
-                store_row(c, c.in(y + start_of<CL>(c, e, u)), o);
+                store_row(c, c.in(y + start_of<CL, WX>(c, e, u)), o);
             }
-        r = next_rows<CL>(r);
-        e = next_start<CL>(c, e);
+        r = next_rows<CL, WX>(r);
+        e = next_start<CL, WX>(c, e);
     };
-    while (full_rows<CL>(r, r1)) {
+    while (full_rows<CL, WX>(r, r1)) {
         rows(Full());
-        if (full_rows<CL>(r, r1)) request(Full());
+        if (full_rows<CL, WX>(r, r1)) request(Full());
     }
     while (r < r1) {
         request(Rest());
@@ -544,6 +551,8 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float 
                     sum[2 * u] = fma(dv, h, sum[2 * u]);
                     sum[2 * u + 1] += dv;
                 }
+                // a row's values are made doubles when it is its turn, not all rows' ahead (registers)
+                asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(p[2]), "+v"(p[3]), "+v"(q[0]), "+v"(q[1]), "+v"(q[2]), "+v"(q[3]));
             }
         int first;
         bool keep;
@@ -568,7 +577,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float 
 }
 
 // rs.part: not NULL in the last launch over the tiles of a block with more than one across.
-template <int CL, bool SMALL, bool PAST, class Block>
+template <int CL, bool SMALL, bool PAST, bool READY, class Block>
 __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float *dy, const Block x, const double *__restrict__ stats, const float *__restrict__ gamma,
                                                                   const NormArgs a, const double2 *__restrict__ part, float *dx, const RowSums rs)
 {
@@ -615,7 +624,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float
     if (full_rows<CL>(r, r1)) request(Full()); // on their way while the sums are added up
     double p[4], q[4]; // dX = (g rstd) dY - p - q x: p and q become those constants of a column
     const double inv = 1.0 / (double)a.n;
-    load_column_sums<CL>(c, part, a.ranges, a.ready, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
+    load_column_sums<CL, READY>(c, part, a.ranges, a.ready, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
         const double k = rstd[v] * q[v];
@@ -653,40 +662,42 @@ static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Tiles: enough workgroups to fill the chip, but not so many ranges that their sums are a load to add up.
 #define PAST_COUNT ((int64_t)48 << 20) // blocks of 200 MB and more are read past the caches
-// From so many values on, the ranges' sums are added up by a launch of their own (4 us); below, every workgroup of the second launch does
-// so for its columns, of fewer ranges.
-#ifndef FINISH_COUNT
-#define FINISH_COUNT (1 << 22)
-#endif
 struct NormPlan {
     NormArgs a;
     int cl;
     bool past;
     size_t row_part, firsts, ready, total; // bytes into the workspace; ready 0: there is none
 };
-static NormPlan plan_norm(int n, int B)
+// The ranges' sums are added up by a launch of their own (4 us), or by every workgroup of the second launch for its columns; then 16 bytes
+// per range and column stand against 4 to 13 per row, and the ranges are fewer, of about sqrt(n) rows.  Own launch / not, us.  Back, from 8
+// bits: 65536 x 64 17.0 / 18.9, 32768 x 64 12.7 / 12.3, 8192 x 2048 50.4 / 56.7, 10007 x 999 38.6 / 43.2, 16384 x 256 17.4 / 15.4, 4096 x 1024 17.1 / 15.1.
+// Forward (where four wavefronts lie beside each other in the second launch then, 4 KB of a row): 16384 x 4096 139 / 150, 8192 x 2048 39.6 / 39.7,
+// 16384 x 256 14.7 / 11.5.
+static NormPlan plan_norm(int n, int B, bool back)
 {
+
     NormPlan p;
     NormArgs &a = p.a;
-    a.n = n; a.B = B;
-    p.past = (int64_t)n * B >= PAST_COUNT;
-    const bool finish = (int64_t)n * B >= FINISH_COUNT;
+    a.n = n; a.B = B; a.ready = nullptr;
+    const int64_t count = (int64_t)n * B;
+    p.past = count >= PAST_COUNT;
+    const bool finish = back ? count >= (B <= 128 ? 4 : 8) << 20 : B >= 4096 && count >= 8 << 20;
+    const int most = finish ? n : std::max(1, (int)std::sqrt(n / (back ? (B <= 128 ? 1.0 : 4.0) : (B <= 128 ? 4.0 : 8.0))));
     int unit;
-    for (p.cl = across(B);; p.cl /= 2) {
+    for (p.cl = across(B);; p.cl /= 2) { // narrower tiles where there would be few of them
         unit = NORM_ROWS * NORM_THREADS / p.cl;
         a.tiles = ceil_div(B, 4 * p.cl);
-        // without that launch: 16 bytes per range and column against 4 per row, and narrower tiles where there would be few
-        const int most = finish ? std::max(1, 512 / a.tiles) : std::max(1, std::min((int)std::sqrt(n / 4.0), 512 / a.tiles));
-        a.rows = std::max(unit, ceil_div(ceil_div(n, most), unit) * unit);
+        a.rows = std::max(unit, ceil_div(ceil_div(n, std::max(1, std::min(most, 512 / a.tiles))), unit) * unit);
         a.ranges = ceil_div(n, a.rows);
         if (finish || p.cl <= 16 || (int64_t)a.tiles * a.ranges >= 256) break;
     }
     a.splits = 1;
-    while (a.splits < 8 && (int64_t)a.ranges * a.tiles * a.splits < 512 && a.rows % (2 * a.splits * unit) == 0) a.splits *= 2;
+    for (int k = 2; k <= 8 && (int64_t)a.ranges * a.tiles * a.splits < 512; ++k) // parts of whole units
+        if (a.rows % (k * unit) == 0) a.splits = k;
     p.row_part = 16 * (size_t)a.ranges * (size_t)B;
-    p.firsts = p.row_part + (a.tiles > 1 ? 16 * (size_t)a.tiles * (size_t)n : 0);
+    p.firsts = p.row_part + (back && a.tiles > 1 ? 16 * (size_t)a.tiles * (size_t)n : 0);
+    p.total = p.firsts + (back ? 0 : 4 * (size_t)B);
     p.ready = 0;
-    p.total = p.firsts + 4 * (size_t)B;
     if (finish) {
         p.ready = (p.total + 15) & ~(size_t)15;
         p.total = p.ready + 16 * (size_t)B;
@@ -694,6 +705,7 @@ static NormPlan plan_norm(int n, int B)
     p.total = (p.total + 255) & ~(size_t)255;
     return p;
 }
+static size_t workspace(int n, int B) { return std::max(plan_norm(n, B, false).total, plan_norm(n, B, true).total); }
 static dim3 norm_grid(const NormArgs &a, int splits) { return dim3((unsigned)(a.tiles * splits * (a.ranges < 8 ? a.ranges : (a.ranges + 7) & ~7))); }
 
 static int check_norm(int32_t n, int32_t B)
@@ -708,7 +720,7 @@ static int check_work(const void *d_work, size_t work_bytes, int32_t n, int32_t 
     if (rc) return rc;
     if (!d_work) return sdnn_fail(SDNN_EINVAL, "d_work is NULL");
     if ((uintptr_t)d_work & 15) return sdnn_fail(SDNN_EINVAL, "d_work must be 16-byte aligned");
-    const size_t need = plan_norm(n, B).total;
+    const size_t need = workspace(n, B);
     if (work_bytes < need) return sdnn_fail(SDNN_ENOMEM, "workspace of %zu bytes, %zu needed", work_bytes, need);
     return SDNN_OK;
 }
@@ -718,15 +730,15 @@ extern "C" int sdnn_layernorm_workspace_bytes(int32_t n, int32_t B, size_t *byte
     if (!bytes) return sdnn_fail(SDNN_EINVAL, "bytes is NULL");
     const int rc = check_norm(n, B);
     if (rc) return rc;
-    *bytes = plan_norm(n, B).total;
+    *bytes = workspace(n, B);
     return SDNN_OK;
 }
 
 // Whether a block takes k_norm_whole: lanes across, or 0.
 static int whole_lanes(int n, int B)
 {
-    if (B < 4 || n > 4096) return 0;
-    return n > 2048 ? ((int64_t)n * B <= 3 << 20 ? 2 : 0) : n <= 1024 && B >= 4096 ? 8 : 4;
+    if (B < 4 || n > 2048 || (n > 1024 && (int64_t)n * B > 16 << 20)) return 0;
+    return n <= 1024 && B >= 4096 ? 8 : 4;
 }
 template <int CL, int ROWS>
 static int forward_whole(const float *x, const float *gamma, const float *beta, int n, int B, double eps, float *y, double *stats, hipStream_t stream)
@@ -745,8 +757,17 @@ static int forward(const float *x, const float *gamma, const float *beta, double
     NormArgs a = pl.a;
     a.ready = pl.ready ? (double2 *)((char *)work + pl.ready) : nullptr;
     hipLaunchKernelGGL((k_norm_sums<CL, SMALL, PAST>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
-    if (a.ready) hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part, firsts, eps, stats);
-    hipLaunchKernelGGL((k_norm_apply<CL, SMALL, PAST>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts, y, stats);
+    if constexpr (CL == 64) {
+        if (a.ready) {
+            hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part, firsts, eps, stats);
+            a.tiles = ceil_div(a.B, 4 * CL * BESIDE);
+            a.splits *= BESIDE / 2;
+            hipLaunchKernelGGL((k_norm_apply<CL, SMALL, PAST, true, BESIDE>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts, y,
+                               stats);
+            return sdnn_launched();
+        }
+    }
+    hipLaunchKernelGGL((k_norm_apply<CL, SMALL, PAST, false, 1>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts, y, stats);
     return sdnn_launched();
 }
 
@@ -757,10 +778,9 @@ extern "C" int sdnn_layernorm(const float *d_X, const float *d_gamma, const floa
     if (rc) return rc;
     if (!d_X || !d_Y) return sdnn_fail(SDNN_EINVAL, "d_X or d_Y is NULL");
     if (!(eps > 0.0) || !(eps <= 1e30)) return sdnn_fail(SDNN_EINVAL, "eps must be > 0");
-    const NormPlan pl = plan_norm(n, B);
+    const NormPlan pl = plan_norm(n, B, false);
     hipStream_t stream = (hipStream_t)stream_;
     switch (whole_lanes(n, B)) {
-    case 2: return forward_whole<2, 8>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, stream);
     case 4:
         return n <= 1024 ? forward_whole<4, 4>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, stream)
                          : forward_whole<4, 8>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, stream);
@@ -786,9 +806,12 @@ static int backward(const float *dy, const Block &x, const double *stats, const 
     a.ready = pl.ready ? (double2 *)((char *)work + pl.ready) : nullptr;
     rs.part = a.tiles > 1 ? (double *)((char *)work + pl.row_part) : nullptr;
     hipLaunchKernelGGL((k_norm_grad_sums<CL, SMALL, PAST, Block>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, rs);
-    if (dx && a.ready) hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part, (const float *)nullptr, 0.0, (double *)nullptr);
-    if (dx || rs.part)
-        hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, PAST, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, dx, rs);
+    if (dx && a.ready) {
+        hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part, (const float *)nullptr, 0.0, (double *)nullptr);
+        hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, PAST, true, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, dx, rs);
+    } else if (dx || rs.part) {
+        hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, PAST, false, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, dx, rs);
+    }
     return sdnn_launched();
 }
 // KIND 0: x; 1 and 2: x8, of values of both signs and of activations
@@ -796,7 +819,7 @@ template <int KIND>
 static int backward_any(const float *dy, const float *x, const PackedArgs &x8, const double *stats, const float *gamma, int n, int B, float *dx, float *dgamma,
                         float *dbeta, void *work, void *stream_)
 {
-    const NormPlan pl = plan_norm(n, B);
+    const NormPlan pl = plan_norm(n, B, true);
     const RowSums rs{nullptr, dgamma, dbeta};
     hipStream_t stream = (hipStream_t)stream_;
     auto go = [&](auto cl, auto small, auto past) {
