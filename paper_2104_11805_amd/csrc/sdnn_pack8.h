@@ -20,31 +20,37 @@
 static inline int64_t pack8_groups(int64_t count) { return (count + PACK_GROUP - 1) / PACK_GROUP; }
 static inline int64_t pack8_bytes(int64_t count) { return ((PACK_GROUP + 2) * pack8_groups(count) + 255) & ~(int64_t)255; }
 
-// The scale of a group whose largest value is `largest`, as the 16 bits that are stored.
-__device__ __forceinline__ unsigned pack8_scale(float largest, float most)
+// The largest value that a group's scale is made for, of those that become multiples of it.
+template <bool SIGNED> __device__ __forceinline__ float pack8_size(float x, float cap)
 {
-    unsigned t = __float_as_uint(largest / most) >> 16; // that, or one or two more: division and cutting off lose
+    if constexpr (SIGNED) return fabsf(x) <= FLT_MAX ? fabsf(x) : 0.0f;
+    return x < cap ? x : 0.0f; // (below zero: less than any largest value; NaN: not less than the cap)
+}
+// The scale of a group whose largest value is `largest`, as the 16 bits that are stored.
+template <bool SIGNED> __device__ __forceinline__ unsigned pack8_scale(float largest)
+{
+    constexpr float most = SIGNED ? 127.0f : 253.0f;
+    unsigned t = __float_as_uint(largest * (1.0f / most)) >> 16; // that, or one or two more: the product and cutting off lose
 #pragma unroll
-    for (int k = 0; k < 2; ++k)
-        if ((double)most * (double)__uint_as_float(t << 16) < (double)largest) ++t;
+    for (int k = 0; k < 2; ++k) t += most * __uint_as_float(t << 16) < largest ? 1u : 0u; // (exact: eight bits times eight)
     return t;
 }
-// What values are multiplied by before they are rounded: 1 / t, and 2^-40 of it more.  The nearest fp32 value to a half of t is 2^-24
-// of it away, so that halves, and nothing else, are lifted over the border that the rounding of this product could move.
+// What values are multiplied by before they are rounded: 1 / t, and 2^-30 of it more.  The fp32 value next to a half of t is 2^-24 of
+// it away, so that the halves, which the product may miss by its rounding, are lifted over the border, and nothing else is.
 __device__ __forceinline__ double pack8_inverse(unsigned t)
 {
-    return t ? (1.0 + 0x1p-40) / (double)__uint_as_float(t << 16) : 0.0;
+    const double d = (double)__uint_as_float(t << 16), r = __builtin_amdgcn_rcp(d); // to 2^-20 and better; one step of Newton's: 2^-40
+    return t ? fma(r, fma(-d, r, 1.0) + 0x1p-30, r) : 0.0;
 }
-__device__ __forceinline__ bool pack8_live(float x, float cap)
+template <bool SIGNED> __device__ __forceinline__ unsigned pack8_code(float x, float cap, double inverse)
 {
-    return cap > 0.0f ? x > 0.0f && x < cap : fabsf(x) <= FLT_MAX;
-}
-__device__ __forceinline__ unsigned pack8_code(float x, float cap, double inverse)
-{
-    const bool live = pack8_live(x, cap);
-    const int c = (int)fma(live ? (double)fabsf(x) : 0.0, inverse, 0.5);
-    if (cap > 0.0f) return live ? (unsigned)max(c, 1) : x >= cap ? 255u : x != x ? 254u : 0u;
-    return live ? (unsigned)(x < 0.0f ? -c : c) & 255u : 128u;
+    if constexpr (SIGNED) {
+        const int c = (int)fma((double)fabsf(x), inverse, 0.5);
+        return fabsf(x) <= FLT_MAX ? (unsigned)(x < 0.0f ? -c : c) & 255u : 128u;
+    }
+    unsigned c = (unsigned)max((int)fma((double)x, inverse, 0.5), 1);
+    c = x > 0.0f ? c : x != x ? 254u : 0u;
+    return x >= cap ? 255u : c;
 }
 // below: the largest float below cap
 template <bool SIGNED> __device__ __forceinline__ float pack8_value_of(unsigned code, float scale, float cap, float below)
