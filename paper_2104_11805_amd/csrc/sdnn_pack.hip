@@ -57,9 +57,9 @@ __global__ void __launch_bounds__(256) k_pack8(const float *__restrict__ x, int6
 }
 
 template <bool SIGNED>
-__global__ void __launch_bounds__(256) k_unpack8(const uint8_t *__restrict__ packed, int64_t count, int64_t groups, float cap, float below, float *__restrict__ x)
+__global__ void __launch_bounds__(256) k_unpack8(const uint8_t *__restrict__ packed, int64_t count, int64_t groups, float cap, float below, float *__restrict__ x, int64_t first)
 {
-    const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t q = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (4 * q >= count) return;
     const unsigned c = reinterpret_cast<const unsigned *>(packed)[q];
     const float t = __uint_as_float((unsigned)reinterpret_cast<const uint16_t *>(packed + PACK_GROUP * groups)[q / (PACK_GROUP / 4)] << 16);
@@ -99,25 +99,39 @@ __device__ __forceinline__ int64_t block_start(const NetBlocks &a, int l, int la
     for (int m = 1; m < 64; m *= 2) bytes += __shfl_xor(bytes, m);
     return bytes;
 }
+// (Loads of several groups or pieces together, at places that are there, without conditions between them.)
 template <bool SIGNED> __device__ __forceinline__ void pack_block(const NetBlocks &a, const float *__restrict__ x, int64_t count, uint8_t *__restrict__ packed)
 {
     const int lane = threadIdx.x & 31;
-    const int64_t groups = (count + PACK_GROUP - 1) / PACK_GROUP;
+    const int64_t groups = (count + PACK_GROUP - 1) / PACK_GROUP, stride = (int64_t)gridDim.x * 8;
     uint16_t *scales = reinterpret_cast<uint16_t *>(packed + PACK_GROUP * groups);
-    for (int64_t g = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); g < groups; g += (int64_t)gridDim.x * 8) {
+    const bool dense = a.ld == a.B;
+    const int64_t wide = dense || (a.B & 3) == 0 ? count / PACK_GROUP : 0; // groups whose fours lie in one piece
+    constexpr int U = 2;
+    int64_t g = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    for (; g < wide; g += U * stride) {
+        F4 f[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t e = PACK_GROUP * min(g + u * stride, wide - 1) + 4 * lane, row = dense ? 0 : quotient(e, a.per_row_inv);
+            f[u] = *reinterpret_cast<const F4 *>(x + (e + row * (a.ld - a.B)));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (g + u * stride < wide) {
+                const float v[4] = {f[u][0], f[u][1], f[u][2], f[u][3]};
+                pack_group<SIGNED>(v, a.cap, lane, packed + PACK_GROUP * (g + u * stride), scales + g + u * stride);
+            }
+    }
+    // the others; each is the next of somebody's
+    for (g = wide + ((int64_t)blockIdx.x * 8 + (threadIdx.x >> 5)); g < groups; g += stride) {
         const int64_t e = PACK_GROUP * g + 4 * lane;
         int64_t row = quotient(e, a.per_row_inv), s = e - row * a.B;
         float v[4];
-        if (s + 4 <= a.B && e + 4 <= count) { // in one row
-            const F4 f = *reinterpret_cast<const F4 *>(x + row * a.ld + s);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = f[k];
-        } else {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[k] = e + k < count ? x[row * a.ld + s] : 0.0f;
-                if (++s == a.B) { s = 0; ++row; }
-            }
+        for (int k = 0; k < 4; ++k) {
+            v[k] = e + k < count ? x[row * a.ld + s] : 0.0f;
+            if (++s == a.B) { s = 0; ++row; }
         }
         pack_group<SIGNED>(v, a.cap, lane, packed + PACK_GROUP * g, scales + g);
     }
@@ -129,38 +143,44 @@ __global__ void __launch_bounds__(256) k_pack_net(const NetBlocks a, int l0)
     if (l == 0) pack_block<true>(a, a.x0, (int64_t)a.layers[0].n_in * a.B, packed);
     else pack_block<false>(a, a.layers[l - 1].X, (int64_t)a.layers[l - 1].n_out * a.B, packed);
 }
-// Columns B .. Bp - 1 become zeros, as the passes leave them.
+// Columns B .. Bp - 1 become zeros, as the passes leave them.  A piece of four samples of a row holds one of the batch at least; the four bytes
+// from its first one on lie in the block, also where they run into its scales.
 template <bool SIGNED> __device__ __forceinline__ void unpack_block(const NetBlocks &a, float *__restrict__ x, int64_t n, const uint8_t *__restrict__ packed)
 {
-    const uint16_t *scales = reinterpret_cast<const uint16_t *>(packed + PACK_GROUP * ((n * a.B + PACK_GROUP - 1) / PACK_GROUP));
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < n * a.per_row; q += (int64_t)gridDim.x * 256) {
-        const int64_t row = quotient(q, a.per_row_inv), s = 4 * (q - row * a.per_row), e = row * a.B + s;
-        const int have = (int)min((int64_t)4, a.B - s), room = (int)min((int64_t)4, a.Bp - s); // have <= 0: filled up only
-        unsigned c = 0;
-        float t[2] = {0.0f, 0.0f};
-        if (have == 4) {
-            c = reinterpret_cast<const U1 *>(packed + e)->v;
-        } else {
+    const int64_t groups = (n * a.B + PACK_GROUP - 1) / PACK_GROUP, pieces = n * a.per_row, stride = (int64_t)gridDim.x * 256;
+    const uint16_t *scales = reinterpret_cast<const uint16_t *>(packed + PACK_GROUP * groups);
+    constexpr int U = 4;
+    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < pieces; q += U * stride) {
+        unsigned c[U];
+        uint16_t t[U][2];
+        int64_t at[U];
+        int have[U], place[U];
 #pragma unroll
-            for (int k = 0; k < 3; ++k)
-                if (k < have) c |= (unsigned)packed[e + k] << (8 * k);
+        for (int u = 0; u < U; ++u) {
+            const int64_t p = min(q + u * stride, pieces - 1), row = quotient(p, a.per_row_inv), s = 4 * (p - row * a.per_row), e = row * a.B + s;
+            have[u] = (int)min((int64_t)4, a.B - s);
+            at[u] = row * a.ld + s;
+            place[u] = (int)(e % PACK_GROUP);
+            c[u] = reinterpret_cast<const U1 *>(packed + e)->v;
+            t[u][0] = scales[e / PACK_GROUP];
+            t[u][1] = scales[(e + have[u] - 1) / PACK_GROUP];
         }
-        if (have > 0) {
-            t[0] = __uint_as_float((unsigned)scales[e / PACK_GROUP] << 16);
-            t[1] = a.B & 3 ? __uint_as_float((unsigned)scales[(e + have - 1) / PACK_GROUP] << 16) : t[0];
-        }
-        const int place = (int)(e % PACK_GROUP);
-        float v[4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            v[k] = k < have ? pack8_value_of<SIGNED>(c >> (8 * k) & 255u, place + k < PACK_GROUP ? t[0] : t[1], a.cap, a.below) : 0.0f;
-        float *out = x + row * a.ld + s;
-        if (room == 4) {
-            *reinterpret_cast<F4 *>(out) = F4{v[0], v[1], v[2], v[3]};
-        } else {
+        for (int u = 0; u < U; ++u) {
+            if (q + u * stride >= pieces) break;
+            float v[4];
 #pragma unroll
-            for (int k = 0; k < 3; ++k)
-                if (k < room) out[k] = v[k];
+            for (int k = 0; k < 4; ++k) {
+                const float scale = __uint_as_float((unsigned)(place[u] + k < PACK_GROUP ? t[u][0] : t[u][1]) << 16);
+                v[k] = k < have[u] ? pack8_value_of<SIGNED>(c[u] >> (8 * k) & 255u, scale, a.cap, a.below) : 0.0f;
+            }
+            if (a.Bp >= 4 * a.per_row) { // room for whole pieces
+                *reinterpret_cast<F4 *>(x + at[u]) = F4{v[0], v[1], v[2], v[3]};
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (k < have[u]) x[at[u] + k] = v[k];
+            }
         }
     }
 }
@@ -182,7 +202,7 @@ int sdnn_launch_checkpoint(const LayerDev *d_layers, float *d_x0, int32_t n_laye
     a.per_row = (Bp + 3) / 4;
     a.per_row_inv = 1.0 / (restore ? a.per_row : B);
     // workgroups that stay: each has to find its block's start first
-    const int64_t work = (max_n * (restore ? 4 * a.per_row : B) + 1023) / 1024;
+    const int64_t work = restore ? (max_n * a.per_row + 1023) / 1024 : (max_n * B + 2047) / 2048;
     const unsigned gx = (unsigned)std::min<int64_t>(std::max<int64_t>(work, 1), std::max(32, 4096 / (n_layers + 1)));
     for (int l0 = 0; l0 <= n_layers; l0 += 65535) {
         const dim3 grid(gx, (unsigned)std::min(65535, n_layers + 1 - l0));
@@ -241,10 +261,13 @@ extern "C" int sdnn_unpack8(const void *d_packed, size_t packed_bytes, int32_t n
     if (rc || n == 0) return rc;
     if (!d_X) return sdnn_fail(SDNN_EINVAL, "d_X is NULL");
     const int64_t count = (int64_t)n * B;
-    const dim3 grid((unsigned)((count + 1023) / 1024));
     const uint8_t *packed = (const uint8_t *)d_packed;
     const float below = nextafterf(cap, 0.0f);
-    if (cap > 0.0f) hipLaunchKernelGGL(k_unpack8<false>, grid, dim3(256), 0, (hipStream_t)stream, packed, count, pack8_groups(count), cap, below, d_X);
-    else hipLaunchKernelGGL(k_unpack8<true>, grid, dim3(256), 0, (hipStream_t)stream, packed, count, pack8_groups(count), cap, below, d_X);
+    const int64_t blocks = (count + 1023) / 1024, most = 1 << 23; // (a launch holds less than 2^32 threads)
+    for (int64_t b = 0; b < blocks; b += most) {
+        const dim3 grid((unsigned)std::min(most, blocks - b));
+        if (cap > 0.0f) hipLaunchKernelGGL(k_unpack8<false>, grid, dim3(256), 0, (hipStream_t)stream, packed, count, pack8_groups(count), cap, below, d_X, 256 * b);
+        else hipLaunchKernelGGL(k_unpack8<true>, grid, dim3(256), 0, (hipStream_t)stream, packed, count, pack8_groups(count), cap, below, d_X, 256 * b);
+    }
     return sdnn_launched();
 }
