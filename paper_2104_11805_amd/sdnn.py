@@ -164,9 +164,8 @@ def sdnn_deal_rows_to_xcds(n_rows, row_ptr, order):
 
 def _stream_ptr(stream=None):
     import torch
-    if stream is None:  # the current one, without making an object of it (2.7 us)
-        return C.c_void_p(_raw_stream())
-    return C.c_void_p(stream.cuda_stream)
+    # the current one without making an object of it (2.7 us)
+    return _raw_stream() if stream is None else stream.cuda_stream
 
 
 def _dp(t):
@@ -346,7 +345,7 @@ class Net:
     def sdnn_weight_grad(self, layer: int, stream=None):
         n_out, _, nnz = self.shapes[layer - 1]
         g, gb = self._empty(nnz), self._empty(n_out)
-        _check(lib().sdnn_weight_grad(self._handle, layer, _dp(g), _dp(gb), _stream_ptr(stream)), self._handle)
+        _check(lib().sdnn_weight_grad(self._handle, layer, g.data_ptr(), gb.data_ptr(), _stream_ptr(stream)), self._handle)
         return g, gb
 
     def sdnn_get_weights(self, layer: int, stream=None):
