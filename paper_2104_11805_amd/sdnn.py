@@ -165,7 +165,7 @@ def sdnn_deal_rows_to_xcds(n_rows, row_ptr, order):
 def _stream_ptr(stream=None):
     import torch
     # the current one without making an object of it (2.7 us)
-    return _raw_stream() if stream is None else stream.cuda_stream
+    return _raw_stream(torch.cuda.current_device()) if stream is None else stream.cuda_stream
 
 
 def _dp(t):
@@ -178,14 +178,17 @@ def _dp(t):
 
 def _tensor(t, name, shape, dtype, index):
     """A device tensor of a call on blocks, after checks of its shape, type, device and layout."""
-    import torch
-    if isinstance(t, torch.Tensor) and t.get_device() == index and t.dtype is dtype and t.shape == shape and t.is_contiguous() and index >= 0:
-        return t
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    try:
+        if t.get_device() == index >= 0 and t.dtype is dtype and t.shape == shape and t.is_contiguous():
+            return t
+        where, what = t.get_device(), f"{t.dtype} {tuple(t.shape)}"
+    except AttributeError:
+        where, what = -1, type(t).__name__
+    if where < 0:
         raise SdnnError(SDNN_EINVAL, f"{name} must be a tensor on the GPU")
-    if t.get_device() != index:
-        raise SdnnError(SDNN_EINVAL, f"{name} is on GPU {t.get_device()}, not on {index}")
-    raise SdnnError(SDNN_EINVAL, f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if where != index:
+        raise SdnnError(SDNN_EINVAL, f"{name} is on GPU {where}, not on {index}")
+    raise SdnnError(SDNN_EINVAL, f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)}, not {what}")
 
 
 def _bytes(t, name, index):
@@ -197,11 +200,11 @@ def _bytes(t, name, index):
 def _block(t, name):
     """n, B and the GPU of a block."""
     import torch
-    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+    index = t.get_device() if isinstance(t, torch.Tensor) and t.dim() == 2 else -1
+    if index < 0:
         raise SdnnError(SDNN_EINVAL, f"{name} must be a two-dimensional tensor on the GPU")
-    _tensor(t, name, t.shape, torch.float32, t.get_device())
-    n, b = t.shape
-    return n, b, t.get_device()
+    n, b = _tensor(t, name, t.shape, torch.float32, index).shape
+    return n, b, index
 
 
 def _elsewhere(index, stream):
@@ -252,6 +255,7 @@ class Net:
                                      _stream_ptr(), C.byref(h)))
         self._handle = h
         self._keep = []
+        self.batch = 0  # samples of the pass that came last
         self.n_layers = len(layers)
         self.shapes = [(l.n_out, l.n_in, int(l.row_ptr[l.n_out])) for l in layers]
         self.total_nnz = sum(s[2] for s in self.shapes)
@@ -271,6 +275,7 @@ class Net:
     def sdnn_forward(self, x0, xl=None, stream=None):
         b = x0.shape[1]
         _check(lib().sdnn_forward(self._handle, _dp(x0), b, _dp(xl), _stream_ptr(stream)), self._handle)
+        self.batch = b
         return xl
 
     def sdnn_forward_noalloc(self, x0, xl, stream=None):
@@ -292,7 +297,7 @@ class Net:
         """sdnn_backward that also forms dJ/dX_0 [n_in(1)][B], in dx0 if it is given."""
         import torch
         n, b, index = _block(dloss, "dloss")
-        _tensor(dloss, "dloss", (self.shapes[-1][0], b), torch.float32, self.index)
+        _tensor(dloss, "dloss", (self.shapes[-1][0], self.batch or b), torch.float32, self.index)
         if (there := _elsewhere(index, stream)) is not None:
             with there:
                 return self.sdnn_backward_input(dloss, dx0)
@@ -311,6 +316,8 @@ class Net:
 
     def sdnn_checkpoint_save(self, b: int, ckpt=None, stream=None):
         """The activations of the forward pass of b samples that came last, in 8 bits (in ckpt, a uint8 tensor, if it is given)."""
+        if b != self.batch and self.batch:
+            raise SdnnError(SDNN_EINVAL, f"the last pass was one of {self.batch} samples, not of {b}")
         if (there := _elsewhere(self.index, stream)) is not None:
             with there:
                 return self.sdnn_checkpoint_save(b, ckpt)
@@ -325,6 +332,7 @@ class Net:
             with there:
                 return self.sdnn_checkpoint_load(ckpt, b)
         _check(lib().sdnn_checkpoint_load(self._handle, _dp(_bytes(ckpt, "ckpt", self.index)), ckpt.numel(), int(b), _stream_ptr()), self._handle)
+        self.batch = int(b)
 
     # -- inspection --
     def _empty(self, *shape, dtype=None):
@@ -381,9 +389,9 @@ def sdnn_gather_probe(table, v: int, idx_i32, n_waves: int, per_wave: int, out, 
 
 # ---- blocks: activations in 8 bits, layer norm -------------------------------------
 
-def _raw_stream() -> int:
+def _raw_stream(index: int) -> int:
     import torch
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _ptr(t):
@@ -412,7 +420,7 @@ def sdnn_pack8(x, cap: float = 0.0, packed=None, stream=None) -> Packed8:
             return sdnn_pack8(x, cap, packed)
     if packed is None:
         packed = torch.empty(sdnn_pack8_bytes(n, b), dtype=torch.uint8, device=x.device)
-    _check(lib().sdnn_pack8(x.data_ptr(), n, b, cap, _bytes(packed, "packed", index).data_ptr(), packed.numel(), _raw_stream()))
+    _check(lib().sdnn_pack8(x.data_ptr(), n, b, cap, _bytes(packed, "packed", index).data_ptr(), packed.numel(), _raw_stream(index)))
     return Packed8(packed, n, b, cap)
 
 
@@ -425,7 +433,7 @@ def sdnn_unpack8(packed: Packed8, x=None, stream=None):
     if x is None:
         x = torch.empty(packed.n, packed.b, device=packed.data.device)
     _tensor(x, "x", (packed.n, packed.b), torch.float32, index)
-    _check(lib().sdnn_unpack8(packed.data.data_ptr(), packed.data.numel(), packed.n, packed.b, packed.cap, x.data_ptr(), _raw_stream()))
+    _check(lib().sdnn_unpack8(packed.data.data_ptr(), packed.data.numel(), packed.n, packed.b, packed.cap, x.data_ptr(), _raw_stream(index)))
     return x
 
 
@@ -456,7 +464,7 @@ def sdnn_layernorm(x, gamma=None, beta=None, eps: float = 1e-5, y=None, stats=No
     work = _work(work, n, b, index)
     y = torch.empty_like(x) if y is None else _tensor(y, "y", (n, b), torch.float32, index)
     stats = torch.empty((2, b), dtype=torch.float64, device=x.device) if stats is None else _tensor(stats, "stats", (2, b), torch.float64, index)
-    _check(lib().sdnn_layernorm(x.data_ptr(), _ptr(gamma), _ptr(beta), n, b, eps, y.data_ptr(), stats.data_ptr(), work.data_ptr(), work.numel(), _raw_stream()))
+    _check(lib().sdnn_layernorm(x.data_ptr(), _ptr(gamma), _ptr(beta), n, b, eps, y.data_ptr(), stats.data_ptr(), work.data_ptr(), work.numel(), _raw_stream(index)))
     return y, stats
 
 
@@ -481,7 +489,7 @@ def sdnn_layernorm_backward(dy, x, stats, gamma=None, dx=None, dgamma=None, dbet
     dx = torch.empty_like(dy) if dx is None else _tensor(dx, "dx", (n, b), torch.float32, index)
     dgamma = dy.new_empty(n) if dgamma is None else _tensor(dgamma, "dgamma", (n,), torch.float32, index)
     dbeta = dy.new_empty(n) if dbeta is None else _tensor(dbeta, "dbeta", (n,), torch.float32, index)
-    out = (n, b, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), work.data_ptr(), work.numel(), _raw_stream())
+    out = (n, b, dx.data_ptr(), dgamma.data_ptr(), dbeta.data_ptr(), work.data_ptr(), work.numel(), _raw_stream(index))
     if packed:
         _check(lib().sdnn_layernorm_backward_packed(dy.data_ptr(), x.data.data_ptr(), x.data.numel(), x.cap, stats.data_ptr(), _ptr(gamma), *out))
     else:

@@ -235,3 +235,24 @@ def test_nets_norms_and_micro_batches_together(widths, b, options):
                 close(host(v), w, bound, stats)
     for net in nets:
         net.close()
+
+
+def test_samples_other_than_those_of_the_pass_are_refused():
+    layers, net, x, dloss, b, activation, cap = make("launch per pass")
+    xd, d = dev(x), dev(dloss)
+    net.sdnn_forward(xd)
+    ckpt = net.sdnn_checkpoint_save(b)
+    for other in (b - 1, b + 1):
+        with pytest.raises(sdnn.SdnnError, match="samples"):
+            net.sdnn_checkpoint_save(other)
+        with pytest.raises(sdnn.SdnnError, match="dloss"):
+            net.sdnn_backward_input(torch.zeros(dloss.shape[0], other, device=DEV))
+    with pytest.raises(sdnn.SdnnError):
+        net.sdnn_forward(dev(wl.normal_inputs(9103, x.shape[0], net.cfg.max_batch + 1)))  # refused: the pass before it is still the last
+    want = net.sdnn_backward_input(d)
+    net.sdnn_forward(dev(wl.normal_inputs(9102, x.shape[0], 3)))
+    with pytest.raises(sdnn.SdnnError, match="needed"):
+        net.sdnn_checkpoint_load(ckpt, b + 16)
+    net.sdnn_checkpoint_load(ckpt, b)
+    assert net.sdnn_backward_input(d).shape == want.shape
+    net.close()
