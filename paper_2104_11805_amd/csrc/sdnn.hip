@@ -2908,9 +2908,12 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_hand_out(const LayerDev *__re
                                                             float *__restrict__ out, int n)
 {
     if ((int)blockIdx.x < bias_blocks) {
-        const int lane = threadIdx.x & 63, row = (int)(blockIdx.x * WAVES_PER_BLOCK + (threadIdx.x >> 6)) * 4 + (lane >> 4);
-        const double sum = bias_gradient(*layer, row, lane & 15, B, ld);
-        if ((lane & 15) == 0 && row < layer->n_out) gb[row] = (float)sum;
+        const int lane = threadIdx.x & 63, n_out = layer->n_out;
+        for (int64_t first = 4 * (blockIdx.x * WAVES_PER_BLOCK + (threadIdx.x >> 6)); first < n_out; first += 4 * (int64_t)bias_blocks * WAVES_PER_BLOCK) {
+            const int row = (int)min(first + (lane >> 4), (int64_t)n_out); // n_out: none
+            const double sum = bias_gradient(*layer, row, lane & 15, B, ld);
+            if ((lane & 15) == 0 && row < n_out) gb[row] = (float)sum;
+        }
         return;
     }
     for (int q = (int)(blockIdx.x - bias_blocks) * BLOCK_THREADS + threadIdx.x; q < n; q += (int)(gridDim.x - bias_blocks) * BLOCK_THREADS) {
@@ -5364,7 +5367,7 @@ extern "C" int sdnn_backward(sdnn_net *net, const float *d_dLoss, void *stream_)
 
 extern "C" int sdnn_backward_input(sdnn_net *net, const float *d_dLoss, float *d_dX0, void *stream_)
 {
-    if (net && !d_dX0) return fail(net, SDNN_EINVAL, "d_dX0 is NULL");
+    if (net && !d_dX0 && net->layers[0].n_in > 0) return fail(net, SDNN_EINVAL, "d_dX0 is NULL");
     return backward_impl(net, d_dLoss, d_dX0, stream_);
 }
 
@@ -5582,7 +5585,7 @@ extern "C" int sdnn_weight_grad(sdnn_net *net, int32_t layer, float *d_g, float 
         const float *g0 = d.G[0], *g1 = net->grad_parts == 2 ? d.G[1] : nullptr;
         const int n = d_g && !spread ? d.nnz : 0;
         if (d_gb && d.n_out > 0) {
-            const int bias_blocks = (d.n_out + 4 * WAVES_PER_BLOCK - 1) / (4 * WAVES_PER_BLOCK);
+            const int bias_blocks = std::min(1 << 20, (d.n_out - 1) / (4 * WAVES_PER_BLOCK) + 1);
             hipLaunchKernelGGL(k_hand_out, dim3((unsigned)(bias_blocks + std::min(4096, (n + BLOCK_THREADS - 1) / BLOCK_THREADS))), dim3(BLOCK_THREADS), 0, stream,
                                net->d_layers + (layer - 1), net->Bp, net->ld, d_gb, bias_blocks, g0, g1, d.t_perm, d_g, n);
         } else if (n > 0) {

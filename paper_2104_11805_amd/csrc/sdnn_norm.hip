@@ -661,6 +661,7 @@ static int across(int B) { return B < 4 ? 1 : B <= 16 ? 4 : B <= 32 ? 8 : B <= 6
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // Tiles: enough workgroups to fill the chip, but not so many ranges that their sums are a load to add up.
+#define MOST_COLUMNS (1 << 26) // of the launches with 32 threads a column: a launch holds less than 2^32
 #define PAST_COUNT ((int64_t)48 << 20) // blocks of 200 MB and more are read past the caches
 struct NormPlan {
     NormArgs a;
@@ -681,7 +682,7 @@ static NormPlan plan_norm(int n, int B, bool back)
     a.n = n; a.B = B; a.ready = nullptr;
     const int64_t count = (int64_t)n * B;
     p.past = count >= PAST_COUNT;
-    const bool finish = back ? count >= (B <= 128 ? 4 : 8) << 20 : B >= 4096 && count >= 8 << 20;
+    const bool finish = B <= MOST_COLUMNS && (back ? count >= (B <= 128 ? 4 : 8) << 20 : B >= 4096 && count >= 8 << 20);
     const int most = finish ? n : std::max(1, (int)std::sqrt(n / (back ? (B <= 128 ? 1.0 : 4.0) : (B <= 128 ? 4.0 : 8.0))));
     int unit;
     for (p.cl = across(B);; p.cl /= 2) { // narrower tiles where there would be few of them
@@ -737,15 +738,15 @@ extern "C" int sdnn_layernorm_workspace_bytes(int32_t n, int32_t B, size_t *byte
 // Whether a block takes k_norm_whole: lanes across, or 0.
 static int whole_lanes(int n, int B)
 {
-    if (B < 4 || n > 2048 || (n > 1024 && (int64_t)n * B > 16 << 20)) return 0;
+    if (B < 4 || B > MOST_COLUMNS || n > 2048 || (n > 1024 && (int64_t)n * B > 16 << 20)) return 0;
     return n <= 1024 && B >= 4096 ? 8 : 4;
 }
 template <int CL, int ROWS>
 static int forward_whole(const float *x, const float *gamma, const float *beta, int n, int B, double eps, float *y, double *stats, hipStream_t stream)
 {
     const dim3 grid((unsigned)ceil_div(B, 4 * CL)), block(WHOLE_THREADS);
-    if (CL > 2 && ROWS > 4 && (int64_t)n * B >= PAST_COUNT)
-        hipLaunchKernelGGL((k_norm_whole<CL, ROWS, (CL > 2 && ROWS > 4)>), grid, block, 0, stream, x, gamma, beta, n, B, eps, 1.0 / (double)n, y, stats);
+    if (CL == 8 && (int64_t)n * B >= PAST_COUNT)
+        hipLaunchKernelGGL((k_norm_whole<CL, ROWS, CL == 8>), grid, block, 0, stream, x, gamma, beta, n, B, eps, 1.0 / (double)n, y, stats);
     else hipLaunchKernelGGL((k_norm_whole<CL, ROWS, false>), grid, block, 0, stream, x, gamma, beta, n, B, eps, 1.0 / (double)n, y, stats);
     return sdnn_launched();
 }

@@ -11,7 +11,7 @@ PTR = """
         size = C.c_size_t()
         def call(name, *args):
             stub.stub_clear()
-            rc = getattr(lib, name)(*[C.c_void_p(a) if isinstance(a, int) and a >= 1 << 32 else a for a in args])
+            rc = getattr(lib, name)(*[C.c_void_p(a) if isinstance(a, int) and a >= 1 << 41 else a for a in args])
             return rc, [l for l in stub.stub_log().decode().split("\\n") if l]
         def refused(code, text, name, *args):
             rc, log = call(name, *args)
@@ -74,6 +74,22 @@ def test_layer_norm_refusals():
         refused(-3, "packed", *bwp(a2=p - 1))
         refused(-1, "aligned", *bwp(a1=A[1] + 4))
         refused(-1, "d_packed", *bwp(a1=None))
+    """)
+
+
+def test_sizes_at_the_ends_of_what_is_taken():
+    """Every launch holds less than 2^32 threads and has room in its grid (the stand-in refuses what the runtime does)."""
+    routes.run(PTR + """
+        M = 1 << 30
+        for n, b in [(1, 1), (1, M), (M, 1), (M, 1023), (1023, M), (1000, 1 << 27), (1000, 1 << 26), (1000, (1 << 26) + 1), (2000, 1 << 23), (2100, 1 << 26), (2100, (1 << 26) + 5),
+                     (4, 1 << 28), (300, 1 << 25), (1 << 20, 1 << 19), (1 << 25, 128), (1 << 25, 3), (1 << 24, 17)]:
+            assert lib.sdnn_layernorm_workspace_bytes(n, b, C.byref(size)) == 0
+            w = size.value
+            assert call("sdnn_layernorm", A[0], A[1], A[2], n, b, 1e-5, A[3], A[4], A[5], w, None)[0] == 0, (n, b, sdnn.last_error())
+            assert call("sdnn_layernorm_backward", A[0], A[1], A[2], A[3], n, b, A[4], A[5], A[6], A[7], w, None)[0] == 0, (n, b, sdnn.last_error())
+            assert lib.sdnn_pack8_bytes(n, b, C.byref(size)) == 0
+            assert call("sdnn_layernorm_backward_packed", A[0], A[1], size.value, 2.0, A[2], A[3], n, b, None, A[5], A[6], A[7], w, None)[0] == 0, (n, b, sdnn.last_error())
+            assert call("sdnn_pack8", A[0], n, b, 0.0, A[1], size.value, None)[0] == 0 and call("sdnn_unpack8", A[1], size.value, n, b, 2.0, A[0], None)[0] == 0, (n, b)
     """)
 
 
