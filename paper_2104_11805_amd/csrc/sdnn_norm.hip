@@ -16,22 +16,20 @@
 
 #define NORM_THREADS 512
 #define NORM_ROWS 4
-#define BESIDE 4 // wavefronts that lie beside each other in a second launch over wide rows
 
 typedef float F4 __attribute__((ext_vector_type(4), aligned(4))); // 16 bytes at any multiple of 4
 struct __attribute__((packed, aligned(1))) U1 { unsigned v; }; // 4 bytes anywhere
 
-// BESIDE wavefronts may lie beside each other (CL = 64), each with a tile of its own.
 // A lane's four columns.  They end with the block's last column at the latest: the last lane's first ones may be its neighbour's, and
 // are left out of everything.  SMALL: B < 4, one lane across.
-template <int CL, bool SMALL, int WX = 1> struct Columns {
+template <int CL, bool SMALL> struct Columns {
     static constexpr bool small = SMALL;
     int tile0, B, lane_row;    // lane_row: of the rows that the wavefront has at a time
     int base, first;           // columns base .. base + 3, of which those from `first` on are the lane's own; none if first >= B
     __device__ __forceinline__ Columns(int tile, int B_)
     {
         B = B_;
-        tile0 = (tile * WX + (WX > 1 ? __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) % WX : 0)) * 4 * CL;
+        tile0 = tile * 4 * CL;
         first = tile0 + 4 * (int)(threadIdx.x & (CL - 1));
         base = SMALL ? 0 : min(first, B - 4);
         lane_row = (int)(threadIdx.x & 63) / CL;
@@ -197,19 +195,19 @@ __device__ __forceinline__ void load_column_sums(const C &c, const double2 *__re
 
 // The rows that a wavefront walks: from its first one on 64 / CL at a time, the lane's is lane_row further, and NORM_ROWS times that, row_of<CL>(r,
 // u), are requested together.  r and where that row starts, e, are the same for the wavefront.
-template <int CL, int WX = 1> __device__ __forceinline__ int first_row(int r0) { return r0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) / WX * (64 / CL); }
-template <int CL, int WX = 1> __device__ __forceinline__ int row_of(int r, int u) { return r + u * (NORM_THREADS / CL / WX); }
-template <int CL, int WX = 1> __device__ __forceinline__ int next_rows(int r) { return row_of<CL, WX>(r, NORM_ROWS); }
+template <int CL> __device__ __forceinline__ int first_row(int r0) { return r0 + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * (64 / CL); }
+template <int CL> __device__ __forceinline__ int row_of(int r, int u) { return r + u * (NORM_THREADS / CL); }
+template <int CL> __device__ __forceinline__ int next_rows(int r) { return row_of<CL>(r, NORM_ROWS); }
 // Whether all of them are there.  Then nothing is asked row by row: a condition around a row's loads has the compiler move what is done with
 // them to where they are, and a row waits for the one before it.  Lanes without columns of their own read their neighbours'.
-template <int CL, int WX = 1> __device__ __forceinline__ bool full_rows(int r, int r1) { return row_of<CL, WX>(r, NORM_ROWS - 1) + 64 / CL <= r1; }
+template <int CL> __device__ __forceinline__ bool full_rows(int r, int r1) { return row_of<CL>(r, NORM_ROWS - 1) + 64 / CL <= r1; }
 typedef std::integral_constant<bool, true> Full;
 typedef std::integral_constant<bool, false> Rest;
 // gamma or beta of a row: `other`, which has n values and more, is read where there is none, and dropped where the value is used
 __device__ __forceinline__ float of_row(const float *p, const float *other, int row) { return (p ? p : other)[row]; }
 template <class C> __device__ __forceinline__ size_t first_start(const C &c, int r) { return (size_t)r * (size_t)c.B; }
-template <int CL, int WX = 1, class C> __device__ __forceinline__ size_t start_of(const C &c, size_t e, int u) { return e + (size_t)u * (NORM_THREADS / CL / WX) * (size_t)c.B; }
-template <int CL, int WX = 1, class C> __device__ __forceinline__ size_t next_start(const C &c, size_t e) { return start_of<CL, WX>(c, e, NORM_ROWS); }
+template <int CL, class C> __device__ __forceinline__ size_t start_of(const C &c, size_t e, int u) { return e + (size_t)u * (NORM_THREADS / CL) * (size_t)c.B; }
+template <int CL, class C> __device__ __forceinline__ size_t next_start(const C &c, size_t e) { return start_of<CL>(c, e, NORM_ROWS); }
 
 struct NormArgs {
     int32_t n, B, rows;            // rows of a range
@@ -224,9 +222,9 @@ __device__ __forceinline__ double2 statistics(double2 s, float first, double inv
     return make_double2((double)first + m, 1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));
 }
 
-// stats: forward, [2][B] or NULL; firsts: forward, NULL: back.
+// The ranges' sums (back), added up and divided by n, where the second launch does not do it.
 #define FINISH_COLUMNS 16
-__global__ void __launch_bounds__(512) k_norm_finish(const NormArgs a, const double2 *__restrict__ part, const float *__restrict__ firsts, double eps, double *__restrict__ stats)
+__global__ void __launch_bounds__(512) k_norm_finish(const NormArgs a, const double2 *__restrict__ part)
 {
     __shared__ double2 lds[512];
     const int tid = threadIdx.x, col = (int)blockIdx.x * FINISH_COLUMNS + (tid & (FINISH_COLUMNS - 1));
@@ -241,16 +239,7 @@ __global__ void __launch_bounds__(512) k_norm_finish(const NormArgs a, const dou
         s.y += lds[k].y;
     }
     const double inv = 1.0 / (double)a.n;
-    if (firsts) {
-        s = statistics(s, firsts[col], inv, eps);
-        if (stats) {
-            stats[col] = s.x;
-            stats[a.B + col] = s.y;
-        }
-    } else {
-        s = make_double2(s.x * inv, s.y * inv);
-    }
-    a.ready[col] = s;
+    a.ready[col] = make_double2(s.x * inv, s.y * inv);
 }
 // Which part a workgroup takes.  Workgroup ids go round the XCDs: an XCD takes whole rows of the block (a tile's columns of all rows lie
 // in the same few of an L2's channels), and in the second launch those that it had in the first.  Few ranges: any.
@@ -270,13 +259,13 @@ __device__ __forceinline__ bool find_tile(const NormArgs &a, int splits, int &ti
 
 // part [range][B]: sums of x - x0 and of its square, x0 the sample's first value: nothing cancels where the mean is large.
 // firsts [B]: x0, which the second launch may write its results over.
-template <int CL, bool SMALL, bool PAST>
+template <int CL, bool SMALL>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restrict__ x, const NormArgs a, double2 *__restrict__ part, float *__restrict__ firsts)
 {
     int tile, range, r0, r1;
     if (!find_tile(a, 1, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
-    const PlainBlock<PAST> in{x};
+    const PlainBlock<false> in{x};
     double s1[4] = {}, s2[4] = {};
     float first[4];
 #pragma unroll
@@ -288,7 +277,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restr
     int r = first_row<CL>(r0);
     size_t e = first_start(c, r);
     auto rows = [&](auto full) {
-        typename PlainBlock<PAST>::Raw t[NORM_ROWS];
+        typename PlainBlock<false>::Raw t[NORM_ROWS];
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
             if (full.value || row_of<CL>(r, u) + c.lane_row < r1) in.request(c, start_of<CL>(c, e, u), t[u]);
@@ -309,10 +298,11 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restr
     store_column_sums<CL>(c, s1, s2, part + (size_t)range * a.B);
 }
 
-template <class C> __device__ __forceinline__ void store_row(const C &c, float *p, const float (&o)[4])
+template <bool PAST = true, class C> __device__ __forceinline__ void store_row(const C &c, float *p, const float (&o)[4])
 {
     if (c.whole()) { // (not so for lanes without columns)
-        __builtin_nontemporal_store(F4{o[0], o[1], o[2], o[3]}, reinterpret_cast<F4 *>(p));
+        if constexpr (PAST) __builtin_nontemporal_store(F4{o[0], o[1], o[2], o[3]}, reinterpret_cast<F4 *>(p));
+        else *reinterpret_cast<F4 *>(p) = F4{o[0], o[1], o[2], o[3]};
     } else {
 #pragma unroll
         for (int v = 0; v < 4; ++v)
@@ -320,32 +310,32 @@ template <class C> __device__ __forceinline__ void store_row(const C &c, float *
     }
 }
 
-template <int CL, bool SMALL, bool PAST, bool READY, int WX>
+template <int CL, bool SMALL>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, const float *__restrict__ gamma, const float *__restrict__ beta, const NormArgs a,
                                                              double eps, const double2 *__restrict__ part, const float *__restrict__ firsts, float *y,
                                                              double *__restrict__ stats)
 {
     int tile, range, r0, r1;
     if (!find_tile(a, a.splits, tile, range, r0, r1)) return;
-    const Columns<CL, SMALL, WX> c(tile, a.B);
-    const PlainBlock<PAST> in{x};
-    int r = first_row<CL, WX>(r0);
+    const Columns<CL, SMALL> c(tile, a.B);
+    const PlainBlock<false> in{x};
+    int r = first_row<CL>(r0);
     size_t e = first_start(c, r);
-    typename PlainBlock<PAST>::Raw t[NORM_ROWS];
+    typename PlainBlock<false>::Raw t[NORM_ROWS];
     float g[NORM_ROWS], b[NORM_ROWS];
     auto request = [&](auto full) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (full.value || row_of<CL, WX>(r, u) + c.lane_row < r1) {
-                in.request(c, start_of<CL, WX>(c, e, u), t[u]);
-                g[u] = of_row(gamma, x, row_of<CL, WX>(r, u) + c.lane_row);
-                b[u] = of_row(beta, x, row_of<CL, WX>(r, u) + c.lane_row);
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
+                in.request(c, start_of<CL>(c, e, u), t[u]);
+                g[u] = of_row(gamma, x, row_of<CL>(r, u) + c.lane_row);
+                b[u] = of_row(beta, x, row_of<CL>(r, u) + c.lane_row);
             }
     };
-    if (full_rows<CL, WX>(r, r1)) request(Full()); // on their way while the sums are added up
+    if (full_rows<CL>(r, r1)) request(Full()); // on their way while the sums are added up
     double mean[4], rstd[4];
     const double inv = 1.0 / (double)a.n;
-    load_column_sums<CL, READY>(c, part, a.ranges, a.ready, mean, rstd, [&](int col, double2 s) {
+    load_column_sums<CL, false>(c, part, a.ranges, nullptr, mean, rstd, [&](int col, double2 s) {
         const double2 out = statistics(s, firsts[col], inv, eps);
         if (r0 == 0 && stats) {
             stats[col] = out.x;
@@ -359,19 +349,19 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
     auto rows = [&](auto full) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
-            if (full.value || row_of<CL, WX>(r, u) + c.lane_row < r1) {
+            if (full.value || row_of<CL>(r, u) + c.lane_row < r1) {
                 const double gd = gamma ? (double)g[u] : 1.0, bd = beta ? (double)b[u] : 0.0;
                 float o[4];
 #pragma unroll
                 for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)t[u].v[v], rstd[v], shift[v]), gd, bd);
-                store_row(c, c.in(y + start_of<CL, WX>(c, e, u)), o);
+                store_row(c, c.in(y + start_of<CL>(c, e, u)), o);
             }
-        r = next_rows<CL, WX>(r);
-        e = next_start<CL, WX>(c, e);
+        r = next_rows<CL>(r);
+        e = next_start<CL>(c, e);
     };
-    while (full_rows<CL, WX>(r, r1)) {
+    while (full_rows<CL>(r, r1)) {
         rows(Full());
-        if (full_rows<CL, WX>(r, r1)) request(Full());
+        if (full_rows<CL>(r, r1)) request(Full());
     }
     while (r < r1) {
         request(Rest());
@@ -380,9 +370,10 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
 }
 
 // Blocks of so few rows that a workgroup holds all of them of CL * 4 columns in registers, ROWS per thread: one launch, and every value is read
-// once.
+// once.  LINES: results are stored past the caches, where rows start at multiples of 64 bytes (1024 x 4096 7.8 us, 9.8 through them); elsewhere the parts of a
+// line that two workgroups write have to meet in a cache (1000 x 20001 45.5 us, 64.5 past it).
 #define WHOLE_THREADS 1024
-template <int CL, int ROWS, bool PAST>
+template <int CL, int ROWS, bool LINES>
 __global__ void __launch_bounds__(WHOLE_THREADS) k_norm_whole(const float *x, const float *__restrict__ gamma, const float *__restrict__ beta, int n, int B, double eps,
                                                               double inv, float *y, double *__restrict__ stats)
 {
@@ -394,7 +385,7 @@ __global__ void __launch_bounds__(WHOLE_THREADS) k_norm_whole(const float *x, co
     const int r = __builtin_amdgcn_readfirstlane(tid >> 6) * (64 / CL);
     // all that is read is requested before anything waits for it
     const int lane_first = c.tile0 + (tid & ~3), col = min(lane_first, B - 4) + (tid & 3); // of the statistics that this thread makes
-    typename PlainBlock<PAST>::Raw t[ROWS];
+    typename PlainBlock<false>::Raw t[ROWS];
     float first[4], g[ROWS], b[ROWS], own_first = 0.0f;
     if (tid < CT && lane_first < B) own_first = x[col];
 #pragma unroll
@@ -402,8 +393,7 @@ __global__ void __launch_bounds__(WHOLE_THREADS) k_norm_whole(const float *x, co
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) { // (rows that are not there: the last one again)
         const int row = min(r + u * STEP + c.lane_row, n - 1);
-        const F4 f = PAST ? __builtin_nontemporal_load(reinterpret_cast<const F4 *>(x + (size_t)row * (size_t)B + (size_t)c.base))
-                          : *reinterpret_cast<const F4 *>(x + (size_t)row * (size_t)B + (size_t)c.base);
+        const F4 f = *reinterpret_cast<const F4 *>(x + (size_t)row * (size_t)B + (size_t)c.base);
 #pragma unroll
         for (int v = 0; v < 4; ++v) t[u].v[v] = f[v];
         g[u] = of_row(gamma, x, row);
@@ -461,7 +451,7 @@ __global__ void __launch_bounds__(WHOLE_THREADS) k_norm_whole(const float *x, co
             float o[4];
 #pragma unroll
             for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)t[u].v[v], rstd[v], shift[v]), gd, bd);
-            store_row(c, y + (size_t)row * (size_t)B + (size_t)c.base, o);
+            store_row<LINES>(c, y + (size_t)row * (size_t)B + (size_t)c.base, o);
         }
     }
 }
@@ -660,7 +650,6 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float
 static int across(int B) { return B < 4 ? 1 : B <= 16 ? 4 : B <= 32 ? 8 : B <= 64 ? 16 : B <= 128 ? 32 : 64; } // lanes, CL
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-// Tiles: enough workgroups to fill the chip, but not so many ranges that their sums are a load to add up.
 #define MOST_COLUMNS (1 << 26) // of the launches with 32 threads a column: a launch holds less than 2^32
 #define PAST_COUNT ((int64_t)48 << 20) // blocks of 200 MB and more are read past the caches
 struct NormPlan {
@@ -669,32 +658,40 @@ struct NormPlan {
     bool past;
     size_t row_part, firsts, ready, total; // bytes into the workspace; ready 0: there is none
 };
-// The ranges' sums are added up by a launch of their own (4 us), or by every workgroup of the second launch for its columns; then 16 bytes
-// per range and column stand against 4 to 13 per row, and the ranges are fewer, of about sqrt(n) rows.  Own launch / not, us.  Back, from 8
-// bits: 65536 x 64 17.0 / 18.9, 32768 x 64 12.7 / 12.3, 8192 x 2048 50.4 / 56.7, 10007 x 999 38.6 / 43.2, 16384 x 256 17.4 / 15.4, 4096 x 1024 17.1 / 15.1.
-// Forward (where four wavefronts lie beside each other in the second launch then, 4 KB of a row): 16384 x 4096 139 / 150, 8192 x 2048 39.6 / 39.7,
-// 16384 x 256 14.7 / 11.5.
+// Forward, and back over blocks of less than 7 << 20 values: 256 workgroups in the first launch, one a CU (264 take as long as 512), so the fewest ranges
+// that fill the chip; every workgroup of the second adds up the ranges' sums for its columns, 16 bytes per range and column, which with 256 workgroups
+// grow with the square of the tile's width, so few or narrow blocks have narrow tiles.  us at CL = 8 / 16 / 32 / 64: forward 65536 x 64 11.7 / 15.4 / 17.5 / 24.2,
+// 16384 x 256 11.2 / 12.1 / 15.5 / 28.8, 3001 x 777 15.5 / 10.3 / 10.5 / 12.7, 37984 x 400 36 / 35 / 38 / 47, 16384 x 1024 38.4 / 36.1 / 36.4 / 39.5,
+// 65536 x 1024 140 / 135 / 132 / 136; back (where a row's sums of many tiles have to be joined) 4001 x 160 9.7 / 9.4 / 10.0 / 13.1, 16384 x 256 17.8 / 16.9 /
+// 20.1 / 33.8, 2100 x 3000 55 / 39 / 33 / 30.  As many parts of them as there are with up to 1024 workgroups in the second launch (at 256 / 512 / 1024 / 2048:
+// 262144 x 64 37.8 / 36.9 / 35.8 / 39.9, 16384 x 1024 36.9 / 36.1 / 35.0 / 39.8).
+// Back over larger blocks, two workgroups a CU in both launches, and the ranges' sums by a launch of their own (4 us).  That / the other way: 10007 x 777 from
+// 8 bits 34.4 / 39.8, 5000 x 1500 25.1 / 27.9, 200000 x 40 36.2 / 39.5, 65536 x 1024 157 / 182; 20000 x 400 31.5 / 31.1, 16384 x 256 16.9 / 14.7.
 static NormPlan plan_norm(int n, int B, bool back)
 {
-
     NormPlan p;
     NormArgs &a = p.a;
     a.n = n; a.B = B; a.ready = nullptr;
     const int64_t count = (int64_t)n * B;
     p.past = count >= PAST_COUNT;
-    const bool finish = B <= MOST_COLUMNS && (back ? count >= (B <= 128 ? 4 : 8) << 20 : B >= 4096 && count >= 8 << 20);
-    const int most = finish ? n : std::max(1, (int)std::sqrt(n / (back ? (B <= 128 ? 1.0 : 4.0) : (B <= 128 ? 4.0 : 8.0))));
-    int unit;
-    for (p.cl = across(B);; p.cl /= 2) { // narrower tiles where there would be few of them
-        unit = NORM_ROWS * NORM_THREADS / p.cl;
-        a.tiles = ceil_div(B, 4 * p.cl);
-        a.rows = std::max(unit, ceil_div(ceil_div(n, std::max(1, std::min(most, 512 / a.tiles))), unit) * unit);
-        a.ranges = ceil_div(n, a.rows);
-        if (finish || p.cl <= 16 || (int64_t)a.tiles * a.ranges >= 256) break;
+    const bool finish = back && B <= MOST_COLUMNS && count >= 7 << 20;
+    p.cl = across(B);
+    if (finish) {
+        if (p.cl == 64 && 4 * ceil_div(B, 128) <= 6 * ceil_div(B, 256)) p.cl = 32; // a quarter of the lanes and more would have no columns
+    } else {
+        const bool large = (double)count * B >= 8.6e9;
+        const int widest = back && B >= 2048 ? 64 : large ? 32 : B > (back ? 160 : 256) ? 16 : n < 2048 ? 16 : 8; // (8: ranges of 256 rows and more, one an XCD)
+        p.cl = std::min(p.cl, widest);
     }
+    const int unit = NORM_ROWS * NORM_THREADS / p.cl;
+    a.tiles = ceil_div(B, 4 * p.cl);
+    int ranges = std::max(1, (finish ? 512 : 256) / a.tiles);
+    if (ranges > 8) ranges &= ~7; // as many for each XCD
+    a.rows = ceil_div(ceil_div(n, unit), ranges) * unit;
+    a.ranges = ceil_div(n, a.rows);
     a.splits = 1;
-    for (int k = 2; k <= 8 && (int64_t)a.ranges * a.tiles * a.splits < 512; ++k) // parts of whole units
-        if (a.rows % (k * unit) == 0) a.splits = k;
+    for (int k = 2; k <= 16; ++k) // parts of whole units
+        if (a.rows % (k * unit) == 0 && (int64_t)a.ranges * a.tiles * k <= (finish ? 512 : 1024)) a.splits = k;
     p.row_part = 16 * (size_t)a.ranges * (size_t)B;
     p.firsts = p.row_part + (back && a.tiles > 1 ? 16 * (size_t)a.tiles * (size_t)n : 0);
     p.total = p.firsts + (back ? 0 : 4 * (size_t)B);
@@ -735,40 +732,30 @@ extern "C" int sdnn_layernorm_workspace_bytes(int32_t n, int32_t B, size_t *byte
     return SDNN_OK;
 }
 
-// Whether a block takes k_norm_whole: lanes across, or 0.
+// Whether a block takes k_norm_whole: lanes across, or 0.  That / two launches, us: 1024 x 64 4.9 / 6.7, 1024 x 4096 7.8 / 11.6, 1000 x 70000 134 / 176,
+// 2000 x 2000 8.9 / 11.3, 2048 x 6000 27.1 / 31.5, 2048 x 8192 45.7 / 35.1; with few rows most of a workgroup is idle: 64 x 2048 3.9 / 6.2, 100 x 10000
+// 7.9 / 8.0, 100 x 100000 49.8 / 26.8.  Up to 1024 rows over 4096 columns and more 32 columns a workgroup, whole lines, and 8 rows a thread.
 static int whole_lanes(int n, int B)
 {
-    if (B < 4 || B > MOST_COLUMNS || n > 2048 || (n > 1024 && (int64_t)n * B > 16 << 20)) return 0;
+    if (B < 4 || B > MOST_COLUMNS || n > 2048 || (n > 1024 && (int64_t)n * B >= 16 << 20) || (n < 128 && B > 8192)) return 0;
     return n <= 1024 && B >= 4096 ? 8 : 4;
 }
 template <int CL, int ROWS>
 static int forward_whole(const float *x, const float *gamma, const float *beta, int n, int B, double eps, float *y, double *stats, hipStream_t stream)
 {
     const dim3 grid((unsigned)ceil_div(B, 4 * CL)), block(WHOLE_THREADS);
-    if (CL == 8 && (int64_t)n * B >= PAST_COUNT)
-        hipLaunchKernelGGL((k_norm_whole<CL, ROWS, CL == 8>), grid, block, 0, stream, x, gamma, beta, n, B, eps, 1.0 / (double)n, y, stats);
+    if (B % 16 == 0) hipLaunchKernelGGL((k_norm_whole<CL, ROWS, true>), grid, block, 0, stream, x, gamma, beta, n, B, eps, 1.0 / (double)n, y, stats);
     else hipLaunchKernelGGL((k_norm_whole<CL, ROWS, false>), grid, block, 0, stream, x, gamma, beta, n, B, eps, 1.0 / (double)n, y, stats);
     return sdnn_launched();
 }
-template <int CL, bool SMALL, bool PAST>
+template <int CL, bool SMALL>
 static int forward(const float *x, const float *gamma, const float *beta, double eps, float *y, double *stats, void *work, const NormPlan &pl, hipStream_t stream)
 {
     double2 *part = (double2 *)work;
     float *firsts = (float *)((char *)work + pl.firsts);
-    NormArgs a = pl.a;
-    a.ready = pl.ready ? (double2 *)((char *)work + pl.ready) : nullptr;
-    hipLaunchKernelGGL((k_norm_sums<CL, SMALL, PAST>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
-    if constexpr (CL == 64) {
-        if (a.ready) {
-            hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part, firsts, eps, stats);
-            a.tiles = ceil_div(a.B, 4 * CL * BESIDE);
-            a.splits *= BESIDE / 2;
-            hipLaunchKernelGGL((k_norm_apply<CL, SMALL, PAST, true, BESIDE>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts, y,
-                               stats);
-            return sdnn_launched();
-        }
-    }
-    hipLaunchKernelGGL((k_norm_apply<CL, SMALL, PAST, false, 1>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts, y, stats);
+    const NormArgs &a = pl.a;
+    hipLaunchKernelGGL((k_norm_sums<CL, SMALL>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, x, a, part, firsts);
+    hipLaunchKernelGGL((k_norm_apply<CL, SMALL>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, x, gamma, beta, a, eps, part, firsts, y, stats);
     return sdnn_launched();
 }
 
@@ -788,14 +775,11 @@ extern "C" int sdnn_layernorm(const float *d_X, const float *d_gamma, const floa
     case 8: return forward_whole<8, 8>(d_X, d_gamma, d_beta, n, B, eps, d_Y, d_stats, stream);
     }
     switch (pl.cl) {
-    case 1: return forward<1, true, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    case 4: return forward<4, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    case 8: return forward<8, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    case 16: return forward<16, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    case 32: return forward<32, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    default:
-        if (pl.past) return forward<64, false, true>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-        return forward<64, false, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 1: return forward<1, true>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 4: return forward<4, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 8: return forward<8, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 16: return forward<16, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    default: return forward<32, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
     }
 }
 
@@ -808,7 +792,7 @@ static int backward(const float *dy, const Block &x, const double *stats, const 
     rs.part = a.tiles > 1 ? (double *)((char *)work + pl.row_part) : nullptr;
     hipLaunchKernelGGL((k_norm_grad_sums<CL, SMALL, PAST, Block>), norm_grid(a, 1), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, rs);
     if (dx && a.ready) {
-        hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part, (const float *)nullptr, 0.0, (double *)nullptr);
+        hipLaunchKernelGGL(k_norm_finish, dim3((unsigned)ceil_div(a.B, FINISH_COLUMNS)), dim3(512), 0, stream, a, part);
         hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, PAST, true, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, dx, rs);
     } else if (dx || rs.part) {
         hipLaunchKernelGGL((k_norm_grad_apply<CL, SMALL, PAST, false, Block>), norm_grid(a, a.splits), dim3(NORM_THREADS), 0, stream, dy, x, stats, gamma, a, part, dx, rs);

@@ -12,9 +12,10 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 # one launch and two: rows 1024 | 1025 and 2048 | 2049, columns 3 | 4 and 4095 | 4096, 2^24 values, 200 MB
 BORDERS = [(1024, 3), (1024, 4), (1024, 5), (1023, 17), (1025, 4), (1025, 19), (2048, 9), (2049, 9), (1024, 4095), (1000, 4096), (1024, 4099), (1, 4097), (2, 8191),
-           (2048, 8192), (2047, 8203), (960, 52430)]
+           (127, 8192), (127, 8193), (128, 8193), (2048, 8192), (2047, 8203), (2047, 8193), (1000, 20001), (960, 52430)]
 # the ranges' sums by a launch of their own, with a last tile that is not whole, tiles of each width, and their neighbours without that launch
-SPLITS = [(70001, 61), (140003, 30), (65536, 64), (65535, 64), (32771, 129), (8192, 1030), (8111, 1037), (2100, 4099), (2500, 4095), (2049, 4096), (524289, 16), (300001, 3),
+SPLITS = [(70001, 61), (140003, 30), (65536, 64), (65535, 64), (32771, 129), (8192, 1030), (8111, 1037), (2100, 4099), (2500, 4095), (2049, 4096), (524289, 16), (300001, 3), (57344, 128), (57343, 128),
+          (24001, 306), (2100, 2101), (4001, 161), (4001, 160), (2047, 500), (200000, 40),
           (1 << 20, 2), (5000001, 1), (40001, 7)]
 FAR = [(2101, 24001), (50331648, 1), (786433, 64)]  # 200 MB and more
 BEHIND = 1 << 16
