@@ -10,23 +10,23 @@
 typedef float F4 __attribute__((ext_vector_type(4), aligned(4))); // 16 bytes at any multiple of 4
 struct __attribute__((packed, aligned(1))) U1 { unsigned v; };     // 4 bytes anywhere
 
-// The largest of a value over a half of the wavefront, in all of its lanes.
-__device__ __forceinline__ float largest_of_half(float v)
+// The largest of a value >= 0, as bits, over a half of the wavefront, in all of its lanes.  (Whole numbers: the exchange is part of the comparison.)
+__device__ __forceinline__ unsigned largest_of_half(unsigned v)
 {
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x128, 0xf, 0xf, true))); // row_ror:8
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x141, 0xf, 0xf, true))); // row_half_mirror
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x4e, 0xf, 0xf, true)));  // quad_perm
-    v = fmaxf(v, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0xb1, 0xf, 0xf, true)));
-    const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x128, 0xf, 0xf, true)); // row_ror:8
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true)); // row_half_mirror
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));  // quad_perm
+    v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));
+    const auto t = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return max(t[0], t[1]);
 }
 // A wavefront's half packs one group: lane g of 32 holds its values 4 g .. 4 g + 3.
 template <bool SIGNED> __device__ __forceinline__ void pack_group(const float (&x)[4], float cap, int lane, uint8_t *codes, uint16_t *scale)
 {
-    float largest = 0.0f;
+    int largest = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) largest = fmaxf(largest, pack8_size<SIGNED>(x[k], cap));
-    const unsigned t = pack8_scale<SIGNED>(largest_of_half(largest));
+    for (int k = 0; k < 4; ++k) largest = max(largest, __float_as_int(pack8_size<SIGNED>(x[k], cap))); // (below zero: less than zero as bits too)
+    const unsigned t = pack8_scale<SIGNED>(__uint_as_float(largest_of_half((unsigned)largest)));
     const double inverse = pack8_inverse(t);
     unsigned c = 0;
 #pragma unroll
@@ -35,27 +35,38 @@ template <bool SIGNED> __device__ __forceinline__ void pack_group(const float (&
     if (lane == 0) *scale = (uint16_t)t;
 }
 
-// What bounds it: 4 bytes read and one written a value, and some 20 instructions.
+// What bounds it: 4 bytes read and one written a value.  A wavefront's half has two groups of the workgroup's stretch of 8 KB requested at a time, and reads past
+// the caches, so that they are left to the codes.  With k_unpack8 after it, 65536 x 1024 110 us (6.1 TB/s), 65536 x 4096 436; through the caches 111 and 489, one
+// group at a time strided by the grid 115 and 560.  Codes stored past the caches as well: k_pack8 59 -> 56 us, but k_unpack8 47 -> 67.
 template <bool SIGNED>
 __global__ void __launch_bounds__(256) k_pack8(const float *__restrict__ x, int64_t count, int64_t groups, float cap, uint8_t *__restrict__ packed)
 {
     const int lane = threadIdx.x & 31;
     uint16_t *scales = reinterpret_cast<uint16_t *>(packed + PACK_GROUP * groups);
-    for (int64_t g = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); g < groups; g += (int64_t)gridDim.x * 8) {
-        const int64_t e = PACK_GROUP * g + 4 * lane;
+    constexpr int U = 2, NEXT = 8;
+    const int64_t whole = count / PACK_GROUP;
+    int64_t g = (int64_t)blockIdx.x * (U * NEXT) + (threadIdx.x >> 5);
+    for (; g < whole; g += (int64_t)gridDim.x * (U * NEXT)) {
+        F4 f[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) f[u] = __builtin_nontemporal_load(reinterpret_cast<const F4 *>(x + (PACK_GROUP * min(g + u * NEXT, whole - 1) + 4 * lane)));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (g + u * NEXT < whole) {
+                const float v[4] = {f[u][0], f[u][1], f[u][2], f[u][3]};
+                pack_group<SIGNED>(v, cap, lane, packed + PACK_GROUP * (g + u * NEXT), scales + g + u * NEXT);
+            }
+    }
+    if (whole < groups && blockIdx.x == 0 && threadIdx.x < 32) { // the block's end: zeros after it
+        const int64_t e = PACK_GROUP * whole + 4 * lane;
         float v[4];
-        if (e + 4 <= count) {
-            const F4 f = *reinterpret_cast<const F4 *>(x + e);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = f[k];
-        } else { // the block's end: zeros after it
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[k] = e + k < count ? x[e + k] : 0.0f;
-        }
-        pack_group<SIGNED>(v, cap, lane, packed + PACK_GROUP * g, scales + g);
+        for (int k = 0; k < 4; ++k) v[k] = e + k < count ? x[e + k] : 0.0f;
+        pack_group<SIGNED>(v, cap, lane, packed + PACK_GROUP * whole, scales + whole);
     }
 }
 
+// One piece of four values a thread, stored past the caches.  What bounds it: one byte read and 4 written a value; 65536 x 1024 47 us (7.2 TB/s).
 template <bool SIGNED>
 __global__ void __launch_bounds__(256) k_unpack8(const uint8_t *__restrict__ packed, int64_t count, int64_t groups, float cap, float below, float *__restrict__ x, int64_t first)
 {
@@ -249,7 +260,7 @@ extern "C" int sdnn_pack8(const float *d_X, int32_t n, int32_t B, float cap, voi
     if (rc || n == 0) return rc;
     if (!d_X) return sdnn_fail(SDNN_EINVAL, "d_X is NULL");
     const int64_t count = (int64_t)n * B;
-    const dim3 grid((unsigned)std::min<int64_t>((pack8_groups(count) + 7) / 8, 8192)); // (a group for each half, 67 million values: 85 us instead of 75)
+    const dim3 grid((unsigned)std::min<int64_t>((pack8_groups(count) + 15) / 16, 16384)); // (8192: 2 us more of 59, no bound: 5 more)
     if (cap > 0.0f) hipLaunchKernelGGL(k_pack8<false>, grid, dim3(256), 0, (hipStream_t)stream, d_X, count, pack8_groups(count), cap, (uint8_t *)d_packed);
     else hipLaunchKernelGGL(k_pack8<true>, grid, dim3(256), 0, (hipStream_t)stream, d_X, count, pack8_groups(count), cap, (uint8_t *)d_packed);
     return sdnn_launched();

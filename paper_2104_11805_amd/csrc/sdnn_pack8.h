@@ -60,10 +60,6 @@ template <bool SIGNED> __device__ __forceinline__ float pack8_value_of(unsigned 
     v = code == 254u ? __builtin_nanf("") : v;
     return code == 255u ? cap : v;
 }
-__device__ __forceinline__ float pack8_value(unsigned code, float scale, float cap, float below)
-{
-    return cap > 0.0f ? pack8_value_of<false>(code, scale, cap, below) : pack8_value_of<true>(code, scale, cap, below);
-}
 
 // ---- host side, shared by the operators on single blocks ----------------------------------------------------------------
 template <class... A> static inline int sdnn_fail(int code, const char *fmt, A... a)
