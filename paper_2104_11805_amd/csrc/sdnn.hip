@@ -1543,7 +1543,8 @@ __global__ void __launch_bounds__(256) k_train_turn(const LayerDev *__restrict__
     }
 }
 
-// And from X_l back to [step][max_batch][position], where the backward pass reads it, after X_l came from a checkpoint.
+// And from X_l back to [step][max_batch][position], where the backward pass reads it, after X_l came from a checkpoint.  120 layers of 1024 neurons, 64
+// samples: 17 us, 3.7 TB/s read and written.
 __global__ void __launch_bounds__(256) k_train_unturn(const LayerDev *__restrict__ layers, int step0, const LmLayer *__restrict__ tab,
                                                       const int32_t *__restrict__ rows, float *__restrict__ to, int max_batch, int ld, int B)
 {
@@ -2902,7 +2903,8 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_apply_bias(const LayerDev *__
     }
 }
 // What sdnn_weight_grad hands out, in one launch: the first bias_blocks workgroups the biases' gradient (16 rows each), the others that of
-// the entries as k_sum_parts does (n = 0: not that).  4096 rows of 32 entries, 128 samples: 5.9 + 5.6 us in two launches of 64 workgroups each.
+// the entries as k_sum_parts does (n = 0: not that).  4096 rows of 32 entries, 128 samples: 4.2 us, little more than an
+// empty launch; 5.9 + 5.6 in two launches of 64 workgroups each.
 __global__ void __launch_bounds__(BLOCK_THREADS) k_hand_out(const LayerDev *__restrict__ layer, int B, int ld, float *__restrict__ gb, int bias_blocks,
                                                             const float *__restrict__ g0, const float *__restrict__ g1, const int32_t *__restrict__ perm,
                                                             float *__restrict__ out, int n)

@@ -5,6 +5,10 @@
 // second adds up the sums of the tiles above and below (back: to the left and right) and writes the result.  A lane holds four
 // neighbouring columns, CL lanes lie across a tile, the others of a wavefront over the rows; NORM_ROWS rows per thread are requested
 // at a time.  Sums are fp64 and in a fixed order, a result is rounded once.
+//
+// What bounds it: the block is read twice (one that the chip's registers do not hold has to be, and the caches give the second reading no more than
+// memory does), 12 bytes a value forward, 20 back, 14.03 back from 8 bits.  16384 x 4096 forward 128 us, 6.3 TB/s of them; 8192 x 2048 back from 8 bits 44 us,
+// 5.4 TB/s.  Blocks of up to a few hundred thousand values: two launches (an empty one 3.5 us) and two chains of loads.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -222,7 +226,7 @@ __device__ __forceinline__ double2 statistics(double2 s, float first, double inv
     return make_double2((double)first + m, 1.0 / sqrt((var < 0.0 ? 0.0 : var) + eps));
 }
 
-// The ranges' sums (back), added up and divided by n, where the second launch does not do it.
+// The ranges' sums (back), added up and divided by n, where the second launch does not do it: 32 threads a column.  8192 x 2048 4.7 us, a launch's time.
 #define FINISH_COLUMNS 16
 __global__ void __launch_bounds__(512) k_norm_finish(const NormArgs a, const double2 *__restrict__ part)
 {
@@ -257,7 +261,8 @@ __device__ __forceinline__ bool find_tile(const NormArgs &a, int splits, int &ti
     return true;
 }
 
-// part [range][B]: sums of x - x0 and of its square, x0 the sample's first value: nothing cancels where the mean is large.
+// part [range][B]: sums of x - x0 and of its square, x0 the sample's first value: nothing cancels where the mean is large (an outlier of a
+// sample of n values is sqrt(n) standard deviations off at most: the variance loses n 2^-53).  16384 x 4096 39 us: 6.9 TB/s.
 // firsts [B]: x0, which the second launch may write its results over.
 template <int CL, bool SMALL>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_sums(const float *__restrict__ x, const NormArgs a, double2 *__restrict__ part, float *__restrict__ firsts)
@@ -310,6 +315,7 @@ template <bool PAST = true, class C> __device__ __forceinline__ void store_row(c
     }
 }
 
+// 16384 x 4096 79 us: 6.8 TB/s, 4 bytes read and 4 written a value.
 template <int CL, bool SMALL>
 __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, const float *__restrict__ gamma, const float *__restrict__ beta, const NormArgs a,
                                                              double eps, const double2 *__restrict__ part, const float *__restrict__ firsts, float *y,
@@ -490,7 +496,8 @@ struct RowSums {
 };
 
 // part [range][B]: sums of g dY and of g dY h over the rows of a range, h = (x - mean) rstd; and the sums of dY h and dY over the
-// tile's columns.
+// tile's columns.  From 8 bits 8192 x 2048 17.5 us: 4.8 TB/s, three fifths of the clocks instructions (seven fp64 ones and three to get a value out of its byte,
+// and eight sums along the rows at a time, halved at every step: seven exchanges for all eight instead of six for each).
 template <int CL, bool SMALL, bool PAST, class Block>
 __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float *__restrict__ dy, const Block x, const double *__restrict__ stats,
                                                                  const float *__restrict__ gamma, const NormArgs a, double2 *__restrict__ part, const RowSums rs)
@@ -566,7 +573,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float 
     store_column_sums<CL>(c, p, q, part + (size_t)range * a.B);
 }
 
-// rs.part: not NULL in the last launch over the tiles of a block with more than one across.
+// rs.part: not NULL in the last launch over the tiles of a block with more than one across.  From 8 bits 8192 x 2048 24 us: 6.3 TB/s.
 template <int CL, bool SMALL, bool PAST, bool READY, class Block>
 __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float *dy, const Block x, const double *__restrict__ stats, const float *__restrict__ gamma,
                                                                   const NormArgs a, const double2 *__restrict__ part, float *dx, const RowSums rs)

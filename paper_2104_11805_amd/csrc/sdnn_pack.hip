@@ -87,6 +87,8 @@ __global__ void __launch_bounds__(256) k_unpack8(const uint8_t *__restrict__ pac
 }
 
 // X_0 .. X_L of a training net, rows of ld floats, to and from one packed block after the other.  grid = (parts, blocks): blockIdx.y + l0 is l.
+// What bounds it: 4 bytes a value on one side, one on the other, after the chain from the layer's record to the block.  4 layers of 65536 neurons, 64 samples 25 us each
+// way (4.2 TB/s), 16384 neurons and 255 samples (rows that are not whole fours) 31 and 26; 8 layers of 4096, 128 samples 8 us.
 struct NetBlocks {
     const LayerDev *layers;
     float *x0;
