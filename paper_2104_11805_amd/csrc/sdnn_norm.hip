@@ -349,9 +349,6 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
         }
         return out;
     });
-    double shift[4]; // h = (x - mean) rstd as x rstd + shift
-#pragma unroll
-    for (int v = 0; v < 4; ++v) shift[v] = -mean[v] * rstd[v];
     auto rows = [&](auto full) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
@@ -359,7 +356,7 @@ __global__ void __launch_bounds__(NORM_THREADS) k_norm_apply(const float *x, con
                 const double gd = gamma ? (double)g[u] : 1.0, bd = beta ? (double)b[u] : 0.0;
                 float o[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)t[u].v[v], rstd[v], shift[v]), gd, bd);
+                for (int v = 0; v < 4; ++v) o[v] = (float)fma(((double)t[u].v[v] - mean[v]) * rstd[v], gd, bd);
                 store_row(c, c.in(y + start_of<CL>(c, e, u)), o);
             }
         r = next_rows<CL>(r);
@@ -442,12 +439,12 @@ __global__ void __launch_bounds__(WHOLE_THREADS) k_norm_whole(const float *x, co
     }
     __syncthreads(); // (and y may be x: everyone has read all that it needs of it)
     if (!c.any()) return;
-    double rstd[4], shift[4];
+    double mean[4], rstd[4];
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
         const double2 s = lds[0][4 * (tid & (CL - 1)) + v];
+        mean[v] = s.x;
         rstd[v] = s.y;
-        shift[v] = -s.x * s.y;
     }
 #pragma unroll
     for (int u = 0; u < ROWS; ++u) {
@@ -456,7 +453,7 @@ __global__ void __launch_bounds__(WHOLE_THREADS) k_norm_whole(const float *x, co
             const double gd = gamma ? (double)g[u] : 1.0, bd = beta ? (double)b[u] : 0.0;
             float o[4];
 #pragma unroll
-            for (int v = 0; v < 4; ++v) o[v] = (float)fma(fma((double)t[u].v[v], rstd[v], shift[v]), gd, bd);
+            for (int v = 0; v < 4; ++v) o[v] = (float)fma(((double)t[u].v[v] - mean[v]) * rstd[v], gd, bd);
             store_row<LINES>(c, y + (size_t)row * (size_t)B + (size_t)c.base, o);
         }
     }
@@ -508,13 +505,13 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float 
     if (!find_tile(a, 1, tile, range, r0, r1)) return;
     const Columns<CL, SMALL> c(tile, a.B);
     const PlainBlock<PAST> up{dy};
-    double p[4] = {}, q[4] = {}, shift[4] = {}, rstd[4] = {}; // h = (x - mean) rstd as x rstd + shift
+    double p[4] = {}, q[4] = {}, mean[4] = {}, rstd[4] = {};
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
         const int col = min(c.base + v, a.B - 1);
-        const double mean = stats[col], k = stats[a.B + col];
-        rstd[v] = c.own(v) ? k : 0.0; // (columns that are not the lane's own must add nothing to the rows' sums)
-        shift[v] = c.own(v) ? -mean * k : 0.0;
+        const double m = stats[col], k = stats[a.B + col];
+        mean[v] = c.own(v) ? m : 0.0; // (columns that are not the lane's own must add nothing to the rows' sums)
+        rstd[v] = c.own(v) ? k : 0.0;
     }
     int r = first_row<CL>(r0);
     size_t e = first_start(c, r);
@@ -542,7 +539,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float 
                         if (!c.own(v)) d[u].v[v] = xv[v] = 0.0f;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
-                    const double h = fma((double)xv[v], rstd[v], shift[v]), dv = (double)d[u].v[v], gd = gr * dv;
+                    const double h = ((double)xv[v] - mean[v]) * rstd[v], dv = (double)d[u].v[v], gd = gr * dv;
                     p[v] += gd;
                     q[v] = fma(gd, h, q[v]);
                     sum[2 * u] = fma(dv, h, sum[2 * u]);
@@ -619,15 +616,11 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float
         rstd[v] = stats[a.B + col];
     }
     if (full_rows<CL>(r, r1)) request(Full()); // on their way while the sums are added up
-    double p[4], q[4]; // dX = (g rstd) dY - p - q x: p and q become those constants of a column
+    double p[4], q[4]; // dX = rstd (g dY - p - (x - mean) q): q becomes that constant of a column
     const double inv = 1.0 / (double)a.n;
     load_column_sums<CL, READY>(c, part, a.ranges, a.ready, p, q, [&](int, double2 s) { return make_double2(s.x * inv, s.y * inv); });
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const double k = rstd[v] * q[v];
-        p[v] = fma(-mean[v] * rstd[v], k, rstd[v] * p[v]);
-        q[v] = rstd[v] * k;
-    }
+    for (int v = 0; v < 4; ++v) q[v] *= rstd[v];
     auto rows = [&](auto full) {
 #pragma unroll
         for (int u = 0; u < NORM_ROWS; ++u)
@@ -637,7 +630,7 @@ __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_apply(const float
                 x.values(c, t[u], xv);
 #pragma unroll
                 for (int v = 0; v < 4; ++v)
-                    o[v] = (float)fma(gr * rstd[v], (double)d[u].v[v], -fma(q[v], (double)xv[v], p[v]));
+                    o[v] = (float)(fma(mean[v] - (double)xv[v], q[v], fma(gr, (double)d[u].v[v], -p[v])) * rstd[v]);
                 store_row(c, c.in(dx + start_of<CL>(c, e, u)), o);
             }
         r = next_rows<CL>(r);

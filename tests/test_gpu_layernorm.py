@@ -86,6 +86,21 @@ def test_a_large_mean_and_samples_without_variance(n, b):
     check_backward(sdnn.sdnn_layernorm_backward(dev(dy), dev(x), stats, dev(gamma)), dy, x, stats.cpu().numpy(), gamma)
 
 
+@pytest.mark.parametrize("eps", [1e-5, 1e-20])
+@pytest.mark.parametrize("n,b", [(1, 5), (500, 7), (1024, 64), (3000, 130), (66000, 130)])
+def test_samples_without_variance_whatever_their_size(n, b, eps):
+    """Every sample is one value n times: h is 0, however large 1/sqrt(eps) is, so that Y is beta, dgamma 0, and dX of a single row 0."""
+    x, gamma, beta, dy = case(n, b, 4)
+    x[:] = (10.0 ** np.linspace(-6, 9, b)).astype(np.float32)
+    y, stats = sdnn.sdnn_layernorm(dev(x), dev(gamma), dev(beta), eps=eps)
+    assert np.array_equal(y.cpu().numpy(), np.broadcast_to(beta[:, None], y.shape))
+    dx, dgamma, dbeta = sdnn.sdnn_layernorm_backward(dev(dy), dev(x), stats, dev(gamma))
+    assert bool((dgamma == 0).all())
+    d = gamma.astype(np.float64)[:, None] * dy
+    want = (d - d.mean(0)) / np.sqrt(eps)
+    close(dx.cpu().numpy(), want, HALF * np.abs(want) + 1e-12 * (np.abs(d) + np.abs(d).mean(0)) / np.sqrt(eps) * (n > 1) + TINY, "dx")
+
+
 @pytest.mark.parametrize("n,b", [(5, 3), (1024, 64), (700, 129), (70000, 12), (64, 2050)])
 @pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
 def test_nonfinite_samples_stay_by_themselves(n, b, bad):
