@@ -224,7 +224,7 @@ int sdnn_backward(sdnn_net *net, const float *d_dLoss, void *stream);
 /* sdnn_backward that also forms the gradient of the net's input, for what comes below the net (a layer norm, another net):
  * d_dX0 [n_in(1)][B] = dJ/dX_0 = W_1^T Delta_1, without a derivative factor (X_0 is no activation of this net's).  Everything else
  * is as after sdnn_backward, to the bit.  Where the sweep of the first layer gathers Delta_1 for the gradient anyway, d_dX0
- * is formed in it; else it is one more product.  d_dX0 must not overlap d_dLoss. */
+ * is formed in it; else it is one more product.  d_dX0 must not overlap d_dLoss (and may be NULL if n_in(1) is 0). */
 int sdnn_backward_input(sdnn_net *net, const float *d_dLoss, float *d_dX0, void *stream);
 
 /* Eqs. 4-5 on every layer, confined to the stored pattern.  Needs a preceding

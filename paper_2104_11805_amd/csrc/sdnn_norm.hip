@@ -493,7 +493,7 @@ struct RowSums {
 };
 
 // part [range][B]: sums of g dY and of g dY h over the rows of a range, h = (x - mean) rstd; and the sums of dY h and dY over the
-// tile's columns.  From 8 bits 8192 x 2048 17.5 us: 4.8 TB/s, three fifths of the clocks instructions (seven fp64 ones and three to get a value out of its byte,
+// tile's columns.  From 8 bits 8192 x 2048 17.5 us: 4.8 TB/s, three fifths of the clocks instructions (eight fp64 ones and three to get a value out of its byte,
 // and eight sums along the rows at a time, halved at every step: seven exchanges for all eight instead of six for each).
 template <int CL, bool SMALL, bool PAST, class Block>
 __global__ void __launch_bounds__(NORM_THREADS, 4) k_norm_grad_sums(const float *__restrict__ dy, const Block x, const double *__restrict__ stats,

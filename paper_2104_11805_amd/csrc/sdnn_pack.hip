@@ -87,8 +87,8 @@ __global__ void __launch_bounds__(256) k_unpack8(const uint8_t *__restrict__ pac
 }
 
 // X_0 .. X_L of a training net, rows of ld floats, to and from one packed block after the other.  grid = (parts, blocks): blockIdx.y + l0 is l.
-// What bounds it: 4 bytes a value on one side, one on the other, after the chain from the layer's record to the block.  4 layers of 65536 neurons, 64 samples 25 us each
-// way (4.2 TB/s), 16384 neurons and 255 samples (rows that are not whole fours) 31 and 26; 8 layers of 4096, 128 samples 8 us.
+// What bounds it: 4 bytes a value on one side, one on the other, after the chain from the layer's record to the block.  4 layers of 65536 neurons, 64 samples 24.6 us
+// into it and 17.9 out of it (4.3 and 5.9 TB/s), 16384 neurons and 255 samples (rows that are not whole fours) 31 and 26; 8 layers of 4096, 128 samples 8.1 and 6.1.
 struct NetBlocks {
     const LayerDev *layers;
     float *x0;
@@ -120,20 +120,20 @@ template <bool SIGNED> __device__ __forceinline__ void pack_block(const NetBlock
     uint16_t *scales = reinterpret_cast<uint16_t *>(packed + PACK_GROUP * groups);
     const bool dense = a.ld == a.B;
     const int64_t wide = dense || (a.B & 3) == 0 ? count / PACK_GROUP : 0; // groups whose fours lie in one piece
-    constexpr int U = 2;
-    int64_t g = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    constexpr int U = 2, NEXT = 8;
+    int64_t g = (int64_t)blockIdx.x * (U * NEXT) + (threadIdx.x >> 5);
     for (; g < wide; g += U * stride) {
         F4 f[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int64_t e = PACK_GROUP * min(g + u * stride, wide - 1) + 4 * lane, row = dense ? 0 : quotient(e, a.per_row_inv);
+            const int64_t e = PACK_GROUP * min(g + u * NEXT, wide - 1) + 4 * lane, row = dense ? 0 : quotient(e, a.per_row_inv);
             f[u] = *reinterpret_cast<const F4 *>(x + (e + row * (a.ld - a.B)));
         }
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (g + u * stride < wide) {
+            if (g + u * NEXT < wide) {
                 const float v[4] = {f[u][0], f[u][1], f[u][2], f[u][3]};
-                pack_group<SIGNED>(v, a.cap, lane, packed + PACK_GROUP * (g + u * stride), scales + g + u * stride);
+                pack_group<SIGNED>(v, a.cap, lane, packed + PACK_GROUP * (g + u * NEXT), scales + g + u * NEXT);
             }
     }
     // the others; each is the next of somebody's
@@ -163,6 +163,28 @@ template <bool SIGNED> __device__ __forceinline__ void unpack_block(const NetBlo
     const int64_t groups = (n * a.B + PACK_GROUP - 1) / PACK_GROUP, pieces = n * a.per_row, stride = (int64_t)gridDim.x * 256;
     const uint16_t *scales = reinterpret_cast<const uint16_t *>(packed + PACK_GROUP * groups);
     constexpr int U = 4;
+    if (a.ld == a.B && (a.B & 3) == 0) { // rows without gaps, of whole fours: as a block
+        for (int64_t q = (int64_t)blockIdx.x * (U * 256) + threadIdx.x; q < pieces; q += U * stride) {
+            unsigned c[U];
+            uint16_t t[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t p = min(q + u * 256, pieces - 1);
+                c[u] = reinterpret_cast<const unsigned *>(packed)[p];
+                t[u] = scales[p / (PACK_GROUP / 4)];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (q + u * 256 >= pieces) break;
+                const float scale = __uint_as_float((unsigned)t[u] << 16);
+                F4 v;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = pack8_value_of<SIGNED>(c[u] >> (8 * k) & 255u, scale, a.cap, a.below);
+                *reinterpret_cast<F4 *>(x + 4 * (q + u * 256)) = v;
+            }
+        }
+        return;
+    }
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < pieces; q += U * stride) {
         unsigned c[U];
         uint16_t t[U][2];
