@@ -194,16 +194,21 @@ def _tensor(t, name, shape, dtype, index):
 def _bytes(t, name, index):
     """The same for a buffer of bytes, whose size the library checks."""
     import torch
-    return _tensor(t, name, (t.numel(),) if isinstance(t, torch.Tensor) else (), torch.uint8, index)
+    return _tensor(t, name, getattr(t, "shape", ()), torch.uint8, index)
 
 
 def _block(t, name):
     """n, B and the GPU of a block."""
     import torch
-    index = t.get_device() if isinstance(t, torch.Tensor) and t.dim() == 2 else -1
+    try:
+        n, b = t.shape
+        index = t.get_device()
+    except (AttributeError, TypeError, ValueError):
+        index = -1
     if index < 0:
         raise SdnnError(SDNN_EINVAL, f"{name} must be a two-dimensional tensor on the GPU")
-    n, b = _tensor(t, name, t.shape, torch.float32, index).shape
+    if t.dtype is not torch.float32 or not t.is_contiguous():
+        _tensor(t, name, (n, b), torch.float32, index)
     return n, b, index
 
 
@@ -447,7 +452,7 @@ def _work(work, n, b, index):
     import torch
     if work is None:
         return torch.empty(sdnn_layernorm_workspace_bytes(n, b), dtype=torch.uint8, device=f"cuda:{index}")
-    return _bytes(work, "work", index)
+    return _tensor(work, "work", getattr(work, "shape", ()), torch.uint8, index)
 
 
 def sdnn_layernorm(x, gamma=None, beta=None, eps: float = 1e-5, y=None, stats=None, work=None, stream=None):
@@ -463,7 +468,7 @@ def sdnn_layernorm(x, gamma=None, beta=None, eps: float = 1e-5, y=None, stats=No
         _tensor(beta, "beta", (n,), torch.float32, index)
     work = _work(work, n, b, index)
     y = torch.empty_like(x) if y is None else _tensor(y, "y", (n, b), torch.float32, index)
-    stats = torch.empty((2, b), dtype=torch.float64, device=x.device) if stats is None else _tensor(stats, "stats", (2, b), torch.float64, index)
+    stats = x.new_empty((2, b), dtype=torch.float64) if stats is None else _tensor(stats, "stats", (2, b), torch.float64, index)
     _check(lib().sdnn_layernorm(x.data_ptr(), _ptr(gamma), _ptr(beta), n, b, eps, y.data_ptr(), stats.data_ptr(), work.data_ptr(), work.numel(), _raw_stream(index)))
     return y, stats
 
