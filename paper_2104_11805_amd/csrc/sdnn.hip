@@ -2622,6 +2622,7 @@ k_update_b1(const LayerDev *__restrict__ layers, int layer0, int lpr_log2, float
 //   eg handles 8 consecutive entries of a 32-entry chunk of the row, sample
 //   lane sg handles samples sg*V + 16*V*t.  A 16-lane butterfly then leaves
 //   the 8 sums of an edge group in 8 different lanes, which write them back.
+//   Of `parts` wavefronts with the same rows (blockIdx.z) each takes every parts-th chunk, the first the biases.
 //   emit == 0: vals -= lr*g, bias -= lr*gb (if update_bias)
 //   emit == 1: g_out / gb_out receive the gradient of the single layer
 // ---------------------------------------------------------------------------
@@ -2629,7 +2630,7 @@ k_update_b1(const LayerDev *__restrict__ layers, int layer0, int lpr_log2, float
 // registers for the whole row (long rows: otherwise it is read again for every 32-entry chunk).
 template <int V, int HOLD>
 __global__ void __launch_bounds__(64 * UPD_WAVES)
-k_update(const LayerDev *__restrict__ layers, int layer0, int n_layers, int interleave, int rows_per_wave, int B, int ld_,
+k_update(const LayerDev *__restrict__ layers, int layer0, int n_layers, int interleave, int rows_per_wave, int parts, int B, int ld_,
          float lr, int update_bias, int emit, float *__restrict__ g_out, float *__restrict__ gb_out)
 {
     // interleaved: grid = (8 * row groups, groups of 8 layers), blockIdx.x % 8 is both the XCD and the
@@ -2651,7 +2652,7 @@ k_update(const LayerDev *__restrict__ layers, int layer0, int n_layers, int inte
     const double dlr = (double)lr;
 
     // bias gradient: sum of the row of Delta over the samples
-    if (emit ? gb_out != nullptr : update_bias != 0) {
+    if (blockIdx.z == 0 && (emit ? gb_out != nullptr : update_bias != 0)) {
         double sum = 0.0;
         for (int s = lane * V; s < B; s += 64 * V) {
             float d[V];
@@ -2683,7 +2684,7 @@ k_update(const LayerDev *__restrict__ layers, int layer0, int n_layers, int inte
             if (s < B) ldv<V>(drow + s, dh[t]);
         }
     }
-    for (int base = beg; base < end; base += 32) {
+    for (int base = beg + 32 * (int)blockIdx.z; base < end; base += 32 * parts) {
         const int p0 = base + eg * 8;
         size_t coff[8];
 #pragma unroll
@@ -5476,27 +5477,36 @@ static int launch_update(sdnn_net *net, int layer0, int n_layers, float lr, int 
         }
         return SDNN_OK;
     }
-    // short rows: a wavefront takes several rows one after the other (fewer, longer-lived wavefronts); long rows: one
+    // Short rows that are more than the chip has room for: a wavefront takes several one after the other (fewer, longer-lived wavefronts; 480 layers of 4096
+    // neurons 2.49 / 2.37 / 2.32 / 2.33 ms for 1 / 2 / 4 / 8), else one.  Fewer rows still: several share a row's chunks, as far as the longest row has them.
+    // One row / four, us: a layer of 352 rows of 32 entries 3.6 / 7.7, 1024 of 32 and 8 layers of them 3.5 / 6.5 and 21.6 / 24.6, 120 layers 138 / 128.
+    // Parts 1 / 4 / 8: 609 rows of 50 entries in the mean, 133 samples 9.4 / 5.5 / 4.8; 4 layers of 1000 rows of 5 to 400 27.0 / 12.9 / -.
     int64_t nnz = 0, rows = 0;
-    for (int l = layer0; l < layer0 + n_layers; ++l) { nnz += net->layers[l].nnz; rows += net->layers[l].n_out; }
-    const int rpw = nnz < 128 * rows ? 4 : 1; // measured on config 2: 2.49 / 2.37 / 2.32 / 2.33 ms for 1 / 2 / 4 / 8
+    int32_t longest = 0;
+    for (int l = layer0; l < layer0 + n_layers; ++l) {
+        nnz += net->layers[l].nnz;
+        rows += net->layers[l].n_out;
+        longest = std::max(longest, net->max_len[0][l]);
+    }
+    const bool short_rows = nnz < 128 * rows;
+    const int rpw = short_rows && rows > 16384 ? 4 : 1, parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(8, (longest + 31) / 32), 16384 / rows));
     const unsigned n_rg = (unsigned)((max_rows + UPD_WAVES * rpw - 1) / (UPD_WAVES * rpw));
     // with many layers, interleave them over the XCDs (one L2 per layer); with few, keep all XCDs on each layer
     const int interleave = n_layers >= 64;
     for (int l0 = 0; l0 < n_layers; l0 += 65535) {
         const int nl = std::min(65535, n_layers - l0);
-        dim3 grid(interleave ? 8u * n_rg : n_rg, (unsigned)(interleave ? (nl + 7) / 8 : nl));
+        dim3 grid(interleave ? 8u * n_rg : n_rg, (unsigned)(interleave ? (nl + 7) / 8 : nl), (unsigned)parts);
         // rows of Delta and X are whole 16-byte pieces, but for the blocks that row_pitch says; long rows: the row of Delta stays
         // in registers
         if (net->ld & 3)
             hipLaunchKernelGGL((k_update<1, 0>), grid, dim3(64 * UPD_WAVES), 0, stream, net->d_layers,
-                               layer0 + l0, nl, interleave, rpw, B, net->ld, lr, net->cfg.update_bias, emit, g, gb);
-        else if (rpw == 1 && B <= 256)
+                               layer0 + l0, nl, interleave, rpw, parts, B, net->ld, lr, net->cfg.update_bias, emit, g, gb);
+        else if (!short_rows && B <= 256)
             hipLaunchKernelGGL((k_update<4, 4>), grid, dim3(64 * UPD_WAVES), 0, stream, net->d_layers,
-                               layer0 + l0, nl, interleave, rpw, B, net->ld, lr, net->cfg.update_bias, emit, g, gb);
+                               layer0 + l0, nl, interleave, rpw, parts, B, net->ld, lr, net->cfg.update_bias, emit, g, gb);
         else
             hipLaunchKernelGGL((k_update<4, 0>), grid, dim3(64 * UPD_WAVES), 0, stream, net->d_layers,
-                               layer0 + l0, nl, interleave, rpw, B, net->ld, lr, net->cfg.update_bias, emit, g, gb);
+                               layer0 + l0, nl, interleave, rpw, parts, B, net->ld, lr, net->cfg.update_bias, emit, g, gb);
         HIP_TRY(net, hipGetLastError());
     }
     return SDNN_OK;

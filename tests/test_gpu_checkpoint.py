@@ -57,6 +57,9 @@ NETS = {
     "separate": ((500, 600, 400), (20, 64), 130, 130, "relu", 2.0, dict(fuse_gradient=-1)),
     "separate, ragged": ((500, 600, 400), (20, 64), 131, 200, "sigmoid", 1.0, dict(fuse_gradient=-1)),
     "separate, long rows": ((600, 500, 400), (300,), 70, 70, "relu", 2.0, dict(fuse_gradient=-1)),
+    "separate, uneven rows": ((600, 500, 400), (5, 5, 0, 40, 300, 31, 33), 29, 64, "relu", 2.0, dict(fuse_gradient=-1)),
+    "separate, uneven rows, two windows": ((609, 500, 609), (5, 64, 400, 5, 65), 133, 133, "relu", 2.0, dict(fuse_gradient=-1)),
+    "separate, many rows": ((900, 17000, 700), (33, 1, 90), 20, 20, "relu", 2.0, dict(fuse_gradient=-1)),
     "panels": ((3000, 2900, 2800), (32, 40), 64, 64, "relu", 2.0, dict(fuse_gradient=-1, panel_cols=512)),
     "panels, ragged": ((3000, 2900, 2800), (32, 40), 77, 90, "relu", 2.0, dict(fuse_gradient=-1, panel_cols=512)),
     "clustered": ((1024, 1024, 1024), (32,), 48, 48, "relu", 2.0, dict(reorder_rows=True)),
