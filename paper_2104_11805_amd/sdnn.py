@@ -307,7 +307,7 @@ class Net:
             with there:
                 return self.sdnn_backward_input(dloss, dx0)
         dx0 = self._empty(self.shapes[0][1], b) if dx0 is None else _tensor(dx0, "dx0", (self.shapes[0][1], b), torch.float32, index)
-        _check(lib().sdnn_backward_input(self._handle, _dp(dloss), _dp(dx0), _stream_ptr()), self._handle)
+        _check(lib().sdnn_backward_input(self._handle, dloss.data_ptr(), dx0.data_ptr(), _raw_stream(index)), self._handle)
         return dx0
 
     def sdnn_sgd_step(self, lr: float, stream=None):
@@ -329,14 +329,14 @@ class Net:
         if ckpt is None:
             import torch
             ckpt = self._empty(self.sdnn_checkpoint_bytes(b), dtype=torch.uint8)
-        _check(lib().sdnn_checkpoint_save(self._handle, _dp(_bytes(ckpt, "ckpt", self.index)), ckpt.numel(), _stream_ptr()), self._handle)
+        _check(lib().sdnn_checkpoint_save(self._handle, _bytes(ckpt, "ckpt", self.index).data_ptr(), ckpt.numel(), _raw_stream(self.index)), self._handle)
         return ckpt
 
     def sdnn_checkpoint_load(self, ckpt, b: int, stream=None):
         if (there := _elsewhere(self.index, stream)) is not None:
             with there:
                 return self.sdnn_checkpoint_load(ckpt, b)
-        _check(lib().sdnn_checkpoint_load(self._handle, _dp(_bytes(ckpt, "ckpt", self.index)), ckpt.numel(), int(b), _stream_ptr()), self._handle)
+        _check(lib().sdnn_checkpoint_load(self._handle, _bytes(ckpt, "ckpt", self.index).data_ptr(), ckpt.numel(), int(b), _raw_stream(self.index)), self._handle)
         self.batch = int(b)
 
     # -- inspection --
