@@ -259,3 +259,27 @@ def test_samples_other_than_those_of_the_pass_are_refused():
     net.sdnn_checkpoint_load(ckpt, b)
     assert net.sdnn_backward_input(d).shape == want.shape
     net.close()
+
+
+@pytest.mark.parametrize("widths,lengths,b", [((70,) * 71, (3, 0, 64, 33), 40), ((130,) * 65, (1, 120, 2), 21), ((40, 300, 40, 300, 40), (40, 2, 2, 2, 300), 200)])
+def test_steps_of_few_rows_in_many_layers(widths, lengths, b):
+    """The separate update where several wavefronts share a row's chunks, of many layers at once and of one: the step takes the gradient
+    that sdnn_weight_grad hands out, and that is the plain form's on the pass's own blocks."""
+    layers = pan_nets.layers(widths, lengths, seed=9400)
+    net = sdnn.Net(layers, 1.0, b, training=True, activation="sigmoid", fuse_gradient=-1, lds_forward=-1)
+    net.sdnn_forward(dev(wl.normal_inputs(9401, widths[0], b)))
+    net.sdnn_backward(dev(wl.normal_inputs(9402, widths[-1], b)))
+    before = [net.sdnn_get_weights(k) for k in range(1, net.n_layers + 1)]
+    grads = [net.sdnn_weight_grad(k) for k in range(1, net.n_layers + 1)]
+    for k, (layer, (g, gb)) in enumerate(zip(layers, grads)):
+        x, delta = (host(t).astype(np.float64) for t in (net.sdnn_get_activation(k, b), net.sdnn_get_delta(k + 1, b)))
+        rows = np.repeat(np.arange(layer.n_out), np.diff(layer.row_ptr))
+        terms = delta[rows] * x[layer.col_idx]
+        close(host(g), terms.sum(1), blocks.HALF * np.abs(terms.sum(1)) + 1e-12 * np.abs(terms).sum(1) + blocks.TINY, f"layer {k + 1}, entries")
+        close(host(gb), delta.sum(1), blocks.HALF * np.abs(delta.sum(1)) + 1e-12 * np.abs(delta).sum(1) + blocks.TINY, f"layer {k + 1}, biases")
+    net.sdnn_sgd_step(0.25)
+    for k in range(net.n_layers):
+        for new, old, g in zip(net.sdnn_get_weights(k + 1), before[k], grads[k]):
+            want = old.double() - 0.25 * g.double()
+            assert bool(((new.double() - want).abs() <= blocks.HALF * want.abs() + 1e-40).all())
+    net.close()
