@@ -651,6 +651,7 @@ static int across(int B) { return B < 4 ? 1 : B <= 16 ? 4 : B <= 32 ? 8 : B <= 6
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 #define MOST_COLUMNS (1 << 26) // of the launches with 32 threads a column: a launch holds less than 2^32
+#define ROW_PAIRS (1 << 29) // columns up to which a wavefront may have two rows: a lane's offset, Columns::in, is 32 bits of bytes from the first of them (and 128 columns a tile of 512 threads make less than 2^32)
 #define PAST_COUNT ((int64_t)48 << 20) // blocks of 200 MB and more are read past the caches by the backward pass (16384 x 4096 244 us, 268 through them; forward 143, 128)
 struct NormPlan {
     NormArgs a;
@@ -680,7 +681,7 @@ static NormPlan plan_norm(int n, int B, bool back)
         if (p.cl == 64 && 4 * ceil_div(B, 128) <= 6 * ceil_div(B, 256)) p.cl = 32; // a quarter of the lanes and more would have no columns
     } else {
         const bool large = (double)count * B >= 8.6e9;
-        const int widest = back && B >= 2048 ? 64 : large ? 32 : B > (back ? 160 : 256) ? 16 : n < 2048 ? 16 : 8; // (8: ranges of 256 rows and more, one an XCD)
+        const int widest = (back && B >= 2048) || B > ROW_PAIRS ? 64 : large ? 32 : B > (back ? 160 : 256) ? 16 : n < 2048 ? 16 : 8; // (8: ranges of 256 rows and more, one an XCD)
         p.cl = std::min(p.cl, widest);
     }
     const int unit = NORM_ROWS * NORM_THREADS / p.cl;
@@ -779,7 +780,8 @@ extern "C" int sdnn_layernorm(const float *d_X, const float *d_gamma, const floa
     case 4: return forward<4, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
     case 8: return forward<8, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
     case 16: return forward<16, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
-    default: return forward<32, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    case 32: return forward<32, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
+    default: return forward<64, false>(d_X, d_gamma, d_beta, eps, d_Y, d_stats, d_work, pl, stream);
     }
 }
 
