@@ -43,11 +43,12 @@ static char arg[92]; // the start of the first argument of the last launch of an
 static char long_arg[80]; // the same for k_fwd_long: the whole argument
 const char *stub_arg() { return arg; }
 const char *stub_long_arg() { return long_arg; }
+static hipError_t last = hipSuccess; // of the launches
 hipError_t hipLaunchKernel(const void *fn, dim3 g, dim3 b, void **args, size_t lds, hipStream_t)
 {
     // what the runtime refuses: 2^32 work items in a dimension, more LDS than a workgroup can have
     if ((unsigned long long)g.x * b.x >= 1ull << 32 || g.y > 65535 || g.z > 65535 || g.x == 0 || g.y == 0 || g.z == 0 || lds > 160 * 1024)
-        return hipErrorInvalidConfiguration;
+        return last = hipErrorInvalidConfiguration;
     if (names()[fn].compare(0, 9, "k_fwd_lds") == 0) memcpy(arg, args[0], sizeof arg);
     if (names()[fn].compare(0, 11, "k_fwd_long<") == 0) memcpy(long_arg, args[0], sizeof long_arg);
     char line[512];
@@ -74,7 +75,12 @@ static int cus = 256;
 void stub_cus(int n) { cus = n; } // nets that are created from now on
 hipError_t hipGetDeviceProperties(hipDeviceProp_t *p, int) { p->multiProcessorCount = cus; return hipSuccess; } // the header appends the version
 const char *hipGetErrorString(hipError_t e) { return e == hipErrorInvalidConfiguration ? "invalid configuration" : "no error"; }
-hipError_t hipGetLastError() { return hipSuccess; }
+hipError_t hipGetLastError() // which a launch by <<<>>> or hipLaunchKernelGGL is asked by
+{
+    const hipError_t e = last;
+    last = hipSuccess;
+    return e;
+}
 hipError_t hipGetSymbolAddress(void **p, const void *) { *p = (void *)((size_t)1 << 44); return hipSuccess; }
 hipError_t hipOccupancyMaxActiveBlocksPerMultiprocessor(int *n, const void *, int, size_t) { *n = 8; return hipSuccess; }
 }

@@ -16,6 +16,48 @@ WIDE = """
 """
 
 
+def test_every_size_that_is_taken_is_launched():
+    """(A launch that the runtime refuses is in no log.)"""
+    routes.run(PTR + WIDE + """
+        for n, b in sizes:
+            for what, (rc, log) in launches(n, b):
+                assert rc == 0, (what, n, b, sdnn.last_error())
+                names = [l.split("<")[0].split()[0] for l in log]
+                if what == "forward":
+                    assert names in (["k_norm_whole"], ["k_norm_sums", "k_norm_apply"]), (what, n, b, log)
+                else:
+                    assert [k for k in names if k != "k_norm_finish"] == ["k_norm_grad_sums", "k_norm_grad_apply"], (what, n, b, log)
+    """)
+
+
+def test_every_packed_block_that_is_taken_is_launched():
+    routes.run(PTR + """
+        M = 1 << 30
+        for n, b in [(1, 1), (1, M), (M, 1), (M, 1023), (1023, M), ((1 << 31) - 1, 511), (1, (1 << 31) - 1), (1 << 20, (1 << 20) - 1)]:
+            assert lib.sdnn_pack8_bytes(n, b, C.byref(size)) == 0, (n, b)
+            for cap in (0.0, 2.0):
+                rc, log = call("sdnn_pack8", A[0], n, b, cap, A[1], size.value, None)
+                assert rc == 0 and len(log) == 1 and log[0].startswith("k_pack8<"), (n, b, rc, log)
+                rc, log = call("sdnn_unpack8", A[1], size.value, n, b, cap, A[0], None)
+                groups = sum(int(l.split()[-3]) for l in log)
+                assert rc == 0 and all(l.startswith("k_unpack8<") for l in log) and groups == -(-n * b // 1024), (n, b, rc, log)
+    """)
+
+
+def test_the_stand_in_remembers_a_launch_that_it_refuses():
+    """As the runtime does: hipGetLastError returns it, once."""
+    routes.run("""
+        class dim3(C.Structure):
+            _fields_ = [("x", C.c_uint32), ("y", C.c_uint32), ("z", C.c_uint32)]
+        stub.hipLaunchKernel.argtypes = [C.c_void_p, dim3, dim3, C.c_void_p, C.c_size_t, C.c_void_p]
+        stub.stub_clear()
+        launch = lambda x, threads: stub.hipLaunchKernel(None, dim3(x, 1, 1), dim3(threads, 1, 1), None, 0, None)
+        assert launch(1 << 23, 512) != 0 and launch(5, 256) == 0
+        assert stub.hipGetLastError() != 0 and stub.hipGetLastError() == 0
+        assert stub.stub_log().decode().split() == ["5", "1", "1"]
+    """)
+
+
 def test_a_lane_finds_its_columns_by_32_bits():
     """A wavefront of a kernel with CL lanes across a tile has 64 / CL rows at a time; the bytes from its first row's start to a lane's four
     columns are a number of 32 bits, and the columns of all rows an int."""
