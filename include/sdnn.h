@@ -244,7 +244,10 @@ int sdnn_sgd_step(sdnn_net *net, float lr, void *stream);
  *   cap = 0  values of both signs, -127 t .. 127 t as signed bytes; -128: infinite or NaN, comes back as NaN
  *   cap > 0  activations 0 <= x <= cap (smaller ones count as 0; cap may be +INFINITY): byte 0: 0; 255: cap; 254: NaN; 1..253: that many t,
  *            for every 0 < x < cap: none becomes 0 or cap, so that f' of the clamped ReLU is exact
- * A value moves by at most t / 2 (with a cap, values below t / 2 by less than t), t <= 1.008 max / 127 or 1.008 max / 253 of its group. */
+ * A value moves by at most t / 2 (with a cap, values below t / 2 by less than t), t <= 1.008 max / 127 or 1.008 max / 253 of its group, and
+ * where that is less than 2^-126 (a subnormal scale), by up to 2^-133 more.  No finite value becomes infinite.
+ * The sigmoid's f' = x (1 - x) has no such bound relative to itself: 1 - x moves as x does, so near 1 (and near 0) by any factor.  A backward pass
+ * from a checkpoint takes the f' of the restored x. */
 
 /* Bytes of a packed block (n >= 0, B >= 1, n B < 2^40; 0 for n = 0). */
 int sdnn_pack8_bytes(int32_t n, int32_t B, size_t *bytes);

@@ -6,8 +6,9 @@
 //   cap == 0  both signs; most = 127: code c stands for c t, -128 for what is not finite
 //   cap > 0   0 <= x <= cap; most = 253: code 0 for 0, 255 for cap, 254 for NaN, and 1 .. 253 for 0 < x < cap (no such value becomes
 //             0, none becomes cap: the derivative of the clamped ReLU is exact)
-// c t is exact in fp32 (8 bits times 8 bits).  A value is off by at most t / 2 <= 0.4 % (cap: 0.2 %) of its group's largest, one
-// below t / 2 with a cap by less than t.
+// c t is exact in fp32 (8 bits times 8 bits), and finite: for the largest floats t is 2^121 (1 + 2/128) at most, of which they are 126.03 (cap: 2^120
+// times that, 252.1), so that the codes whose products would be infinite are not reached.  A value is off by at most t / 2, one below t / 2 with a cap by less
+// than t; t / 2 is 0.4 % (cap: 0.2 %) of the group's largest value, and where t is subnormal (a largest value below 2^-119; cap: 2^-118) up to 2^-134 more.
 #pragma once
 #include <cfloat>
 #include <cstdint>
