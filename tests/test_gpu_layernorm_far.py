@@ -43,3 +43,20 @@ def test_more_columns_than_two_rows_of_them_have_offsets_in_32_bits(n, b):
     lost = 2.0 ** -53 * (b / 1024 + 1000)
     close(dgamma, sums[0], HALF * sums[0].abs() + lost * sums[1], "dgamma")
     close(dbeta, sums[2], HALF * sums[2].abs() + lost * sums[3], "dbeta")
+
+
+def test_dx_over_dy_from_8_bits_behind_32_bits_of_offset():
+    """More than 2^31 values: dX written over dY and formed from the packed block, whole columns of it, at every row."""
+    n, b = 140000, 16384
+    x, y = random((n, b), 5), random((n, b), 6)
+    gamma = random((n,), 7)
+    cols = torch.tensor([0, 5, 255, 256, 8191, 16383], device=DEV)
+    stats = sdnn.sdnn_layernorm(x, gamma)[1]
+    packed = sdnn.sdnn_pack8(x)
+    xd, dyd = sdnn.sdnn_unpack8(packed, x=x)[:, cols].double(), y[:, cols].double()  # (what the bytes stand for: test_gpu_pack8)
+    dx, dgamma, dbeta = sdnn.sdnn_layernorm_backward(y, packed, stats, gamma, dx=y)
+    mean, rstd = stats[:, cols]
+    h, d, most = (xd - mean) * rstd, gamma.double()[:, None] * dyd, (xd.abs() + mean.abs()) * rstd
+    want = rstd * (d - d.mean(0) - h * (d * h).mean(0))
+    bound = rstd * (d.abs() + d.abs().mean(0) + most * (d.abs() * most).mean(0))
+    close(dx[:, cols], want, HALF * want.abs() + 1e-12 * bound, "dx")
