@@ -197,6 +197,14 @@ def _bytes(t, name, index):
     return _tensor(t, name, getattr(t, "shape", ()), torch.uint8, index)
 
 
+def _int32(v, name):
+    """A whole number that the library takes as one of 32 bits (ctypes would cut off the others)."""
+    v = int(v)
+    if not -1 << 31 <= v < 1 << 31:
+        raise SdnnError(SDNN_EINVAL, f"{name} = {v} is past 32 bits")
+    return v
+
+
 def _block(t, name):
     """n, B and the GPU of a block."""
     import torch
@@ -209,6 +217,8 @@ def _block(t, name):
         raise SdnnError(SDNN_EINVAL, f"{name} must be a two-dimensional tensor on the GPU")
     if t.dtype is not torch.float32 or not t.is_contiguous():
         _tensor(t, name, (n, b), torch.float32, index)
+    if (n | b) >> 31:
+        _int32(max(n, b), f"a dimension of {name}")
     return n, b, index
 
 
@@ -316,7 +326,7 @@ class Net:
     # -- activations in 8 bits --
     def sdnn_checkpoint_bytes(self, b: int) -> int:
         n = C.c_size_t(0)
-        _check(lib().sdnn_checkpoint_bytes(self._handle, int(b), C.byref(n)))
+        _check(lib().sdnn_checkpoint_bytes(self._handle, _int32(b, "b"), C.byref(n)))
         return n.value
 
     def sdnn_checkpoint_save(self, b: int, ckpt=None, stream=None):
@@ -333,11 +343,12 @@ class Net:
         return ckpt
 
     def sdnn_checkpoint_load(self, ckpt, b: int, stream=None):
+        b = _int32(b, "b")
         if (there := _elsewhere(self.index, stream)) is not None:
             with there:
                 return self.sdnn_checkpoint_load(ckpt, b)
-        _check(lib().sdnn_checkpoint_load(self._handle, _bytes(ckpt, "ckpt", self.index).data_ptr(), ckpt.numel(), int(b), _raw_stream(self.index)), self._handle)
-        self.batch = int(b)
+        _check(lib().sdnn_checkpoint_load(self._handle, _bytes(ckpt, "ckpt", self.index).data_ptr(), ckpt.numel(), b, _raw_stream(self.index)), self._handle)
+        self.batch = b
 
     # -- inspection --
     def _empty(self, *shape, dtype=None):
@@ -405,7 +416,7 @@ def _ptr(t):
 
 def sdnn_pack8_bytes(n: int, b: int) -> int:
     nbytes = C.c_size_t(0)
-    _check(lib().sdnn_pack8_bytes(int(n), int(b), C.byref(nbytes)))
+    _check(lib().sdnn_pack8_bytes(_int32(n, "n"), _int32(b, "b"), C.byref(nbytes)))
     return nbytes.value
 
 
@@ -414,6 +425,8 @@ class Packed8:
 
     def __init__(self, data, n: int, b: int, cap: float = 0.0):
         self.data, self.n, self.b, self.cap = data, int(n), int(b), float(cap)
+        if (self.n | self.b) >> 31:
+            _int32(self.n, "n"), _int32(self.b, "b")
 
 
 def sdnn_pack8(x, cap: float = 0.0, packed=None, stream=None) -> Packed8:
@@ -444,7 +457,7 @@ def sdnn_unpack8(packed: Packed8, x=None, stream=None):
 
 def sdnn_layernorm_workspace_bytes(n: int, b: int) -> int:
     nbytes = C.c_size_t(0)
-    _check(lib().sdnn_layernorm_workspace_bytes(int(n), int(b), C.byref(nbytes)))
+    _check(lib().sdnn_layernorm_workspace_bytes(_int32(n, "n"), _int32(b, "b"), C.byref(nbytes)))
     return nbytes.value
 
 

@@ -1,0 +1,55 @@
+"""Numbers that the C interface's types cannot hold are refused by the binding, not cut down to others (no GPU: nothing gets as far as a launch)."""
+import pytest
+import torch
+
+from paper_2104_11805_amd import sdnn
+
+
+class Large:
+    """Looks like a block on the GPU of a size that no test has the memory for."""
+    dtype = torch.float32
+
+    def __init__(self, *shape):
+        self.shape = shape
+
+    def get_device(self):
+        return 0
+
+    def is_contiguous(self):
+        return True
+
+
+def refused(text, call, *args, **kw):
+    with pytest.raises(sdnn.SdnnError) as e:
+        call(*args, **kw)
+    assert e.value.code == sdnn.SDNN_EINVAL and text in str(e.value), e.value
+
+
+@pytest.mark.parametrize("large", [1 << 31, 1 << 32, (1 << 32) + 128, -(1 << 32) + 5])
+def test_sizes_past_32_bits(large):
+    for bytes_of in (sdnn.sdnn_pack8_bytes, sdnn.sdnn_layernorm_workspace_bytes):
+        refused(str(large), bytes_of, large, 1)
+        refused(str(large), bytes_of, 1, large)
+    refused(str(large), sdnn.Packed8, None, large, 1)
+    refused(str(large), sdnn.Packed8, None, 1, large)
+    if large < 0:
+        return
+    for shape in ((large, 1), (1, large)):
+        x = Large(*shape)
+        refused(str(large), sdnn.sdnn_pack8, x)
+        refused(str(large), sdnn.sdnn_layernorm, x)
+        refused(str(large), sdnn.sdnn_layernorm_backward, x, x, None)
+
+
+@pytest.mark.parametrize("large", [1 << 32, (1 << 32) + 7])
+def test_batches_of_a_checkpoint_past_32_bits(large):
+    net = object.__new__(sdnn.Net)
+    net._handle, net.batch, net.index = None, 0, 0
+    refused(str(large), net.sdnn_checkpoint_bytes, large)
+    refused(str(large), net.sdnn_checkpoint_load, None, large)
+
+
+def test_what_is_taken():
+    assert sdnn.sdnn_pack8_bytes((1 << 31) - 1, 1) > 1 << 31
+    assert sdnn.Packed8(None, 3, 4).cap == 0.0 and sdnn.Packed8(None, 3, 4, 2.0 ** -149).cap == 2.0 ** -149
+    assert sdnn.Packed8(None, (1 << 31) - 1, 511, float("inf")).b == 511
