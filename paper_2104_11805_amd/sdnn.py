@@ -205,6 +205,14 @@ def _int32(v, name):
     return v
 
 
+def _cap(cap):
+    """A cap as the library takes it, an fp32 number: 0 is another coding, and nothing else may become it."""
+    cap = float(cap)
+    if cap and -2.0 ** -150 <= cap <= 2.0 ** -150:
+        raise SdnnError(SDNN_EINVAL, f"cap = {cap} is 0 in fp32")
+    return cap
+
+
 def _block(t, name):
     """n, B and the GPU of a block."""
     import torch
@@ -424,7 +432,7 @@ class Packed8:
     """A block [n][b] in 8 bits: its bytes (a uint8 tensor) and the cap that they were made with (0: values of both signs)."""
 
     def __init__(self, data, n: int, b: int, cap: float = 0.0):
-        self.data, self.n, self.b, self.cap = data, int(n), int(b), float(cap)
+        self.data, self.n, self.b, self.cap = data, int(n), int(b), _cap(cap)
         if (self.n | self.b) >> 31:
             _int32(self.n, "n"), _int32(self.b, "b")
 
@@ -433,6 +441,7 @@ def sdnn_pack8(x, cap: float = 0.0, packed=None, stream=None) -> Packed8:
     """packed: a uint8 tensor of sdnn_pack8_bytes, or None."""
     import torch
     n, b, index = _block(x, "x")
+    cap = _cap(cap)
     if (there := _elsewhere(index, stream)) is not None:
         with there:
             return sdnn_pack8(x, cap, packed)

@@ -49,6 +49,13 @@ def test_batches_of_a_checkpoint_past_32_bits(large):
     refused(str(large), net.sdnn_checkpoint_load, None, large)
 
 
+@pytest.mark.parametrize("cap", [1e-60, 2.0 ** -150, -1e-60, 5e-324])
+def test_caps_that_are_0_in_fp32(cap):
+    """0 stands for values of both signs: a cap that is rounded to it would take another coding."""
+    refused("cap", sdnn.sdnn_pack8, Large(3, 4), cap)
+    refused("cap", sdnn.Packed8, None, 3, 4, cap)
+
+
 def test_what_is_taken():
     assert sdnn.sdnn_pack8_bytes((1 << 31) - 1, 1) > 1 << 31
     assert sdnn.Packed8(None, 3, 4).cap == 0.0 and sdnn.Packed8(None, 3, 4, 2.0 ** -149).cap == 2.0 ** -149
