@@ -273,7 +273,7 @@ int sdnn_checkpoint_load(sdnn_net *net, const void *d_ckpt, size_t ckpt_bytes, i
  *   dX(i,s) = r_s (gamma(i) dY(i,s) - 1/n sum_k gamma(k) dY(k,s) - h(i,s) 1/n sum_k gamma(k) dY(k,s) h(k,s))
  *   dgamma(i) = sum_s dY(i,s) h(i,s),  dbeta(i) = sum_s dY(i,s)
  * d_gamma, d_beta [n] or NULL (ones, zeros).  d_stats: double [2][B], m and then r, written by the forward pass (NULL: not wanted) and
- * read by the backward pass.  eps > 0.  A sample that holds an infinity or NaN becomes NaN, and no other does.
+ * read by the backward pass.  0 < eps <= 1e30.  A sample that holds an infinity or NaN becomes NaN, and no other does.
  * 1 <= n, B <= 2^30, n B < 2^40.  d_work: sdnn_layernorm_workspace_bytes (SDNN_ENOMEM if work_bytes is less), aligned to 16; its contents
  * do not matter, and calls that share it must be ordered (two graphs that are replayed at a time need one each). */
 int sdnn_layernorm_workspace_bytes(int32_t n, int32_t B, size_t *bytes);

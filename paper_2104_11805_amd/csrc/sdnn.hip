@@ -2866,8 +2866,6 @@ __global__ void __launch_bounds__(256) k_refresh_vals_t(const LayerDev *__restri
     for (int q = blockIdx.x * 256 + threadIdx.x; q < L.nnz; q += gridDim.x * 256) L.vals_t[q] = L.vals[L.t_perm[q]];
 }
 
-// 16 lanes per row, four rows per wavefront at a time, 16 consecutive rows per wavefront.
-// gb_out == NULL: bias -= lr * gb; otherwise the bias gradient of the one layer is stored there instead.
 // The sum of a row of Delta over the samples, by 16 lanes (l: which of them), in all of them.
 __device__ __forceinline__ double bias_gradient(const LayerDev &L, int row, int l, int B, int ld)
 {
@@ -2888,6 +2886,8 @@ __device__ __forceinline__ double bias_gradient(const LayerDev &L, int row, int 
     for (int off = 8; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
     return sum;
 }
+// 16 lanes per row, four rows per wavefront at a time, 16 consecutive rows per wavefront.
+// gb_out == NULL: bias -= lr * gb; otherwise the bias gradient of the one layer is stored there instead.
 __global__ void __launch_bounds__(BLOCK_THREADS) k_apply_bias(const LayerDev *__restrict__ layers, int B, int ld, float lr,
                                                               float *__restrict__ gb_out)
 {

@@ -48,7 +48,7 @@ template <int CL, bool SMALL> struct Columns {
     __device__ __forceinline__ bool ragged() const { return SMALL || tile0 + 4 * CL > B; } // some lane of the tile is not whole (uniform)
 };
 
-// The block that is normalized, as it is ... (PAST: read past the caches, a block that they do not hold)
+// The block that is normalized, as it is ... (PAST: read past the caches)
 template <bool PAST> struct PlainBlock {
     const float *x;
     struct Raw { float v[4]; };
@@ -652,7 +652,7 @@ static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 #define MOST_COLUMNS (1 << 26) // of the launches with 32 threads a column: a launch holds less than 2^32
 #define ROW_PAIRS (1 << 29) // columns up to which a wavefront may have two rows: a lane's offset, Columns::in, is 32 bits of bytes from the first of them (and 128 columns a tile of 512 threads make less than 2^32)
-#define PAST_COUNT ((int64_t)48 << 20) // blocks of 200 MB and more are read past the caches by the backward pass (16384 x 4096 244 us, 268 through them; forward 143, 128)
+#define PAST_COUNT ((int64_t)48 << 20) // blocks of 200 MB and more that have tiles of 256 columns are read past the caches by the backward pass (16384 x 4096 244 us, 268 through them; forward 143, 128)
 struct NormPlan {
     NormArgs a;
     int cl;
@@ -674,7 +674,6 @@ static NormPlan plan_norm(int n, int B, bool back)
     NormArgs &a = p.a;
     a.n = n; a.B = B; a.ready = nullptr;
     const int64_t count = (int64_t)n * B;
-    p.past = count >= PAST_COUNT;
     const bool finish = back && B <= MOST_COLUMNS && count >= 7 << 20;
     p.cl = across(B);
     if (finish) {
@@ -684,6 +683,7 @@ static NormPlan plan_norm(int n, int B, bool back)
         const int widest = (back && B >= 2048) || B > ROW_PAIRS ? 64 : large ? 32 : B > (back ? 160 : 256) ? 16 : n < 2048 ? 16 : 8; // (8: ranges of 256 rows and more, one an XCD)
         p.cl = std::min(p.cl, widest);
     }
+    p.past = back && p.cl == 64 && count >= PAST_COUNT;
     const int unit = NORM_ROWS * NORM_THREADS / p.cl;
     a.tiles = ceil_div(B, 4 * p.cl);
     int ranges = std::max(1, (finish ? 512 : 256) / a.tiles);
@@ -766,7 +766,7 @@ extern "C" int sdnn_layernorm(const float *d_X, const float *d_gamma, const floa
     const int rc = check_work(d_work, work_bytes, n, B);
     if (rc) return rc;
     if (!d_X || !d_Y) return sdnn_fail(SDNN_EINVAL, "d_X or d_Y is NULL");
-    if (!(eps > 0.0) || !(eps <= 1e30)) return sdnn_fail(SDNN_EINVAL, "eps must be > 0");
+    if (!(eps > 0.0) || !(eps <= 1e30)) return sdnn_fail(SDNN_EINVAL, "eps must be > 0 and at most 1e30");
     const NormPlan pl = plan_norm(n, B, false);
     hipStream_t stream = (hipStream_t)stream_;
     switch (whole_lanes(n, B)) {

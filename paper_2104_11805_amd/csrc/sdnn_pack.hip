@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(256) k_unpack8(const uint8_t *__restrict__ pac
 struct NetBlocks {
     const LayerDev *layers;
     float *x0;
-    int32_t n_layers, B, Bp, ld;
+    int32_t B, Bp, ld;
     float cap, below;
     uint8_t *packed;
     int32_t per_row;     // out of a checkpoint: pieces of four samples in a row
@@ -232,7 +232,7 @@ int sdnn_launch_checkpoint(const LayerDev *d_layers, float *d_x0, int32_t n_laye
                            void *d_ckpt, int restore, void *stream)
 {
     NetBlocks a;
-    a.layers = d_layers; a.x0 = d_x0; a.n_layers = n_layers; a.B = B; a.Bp = Bp; a.ld = ld; a.cap = cap; a.below = nextafterf(cap, 0.0f);
+    a.layers = d_layers; a.x0 = d_x0; a.B = B; a.Bp = Bp; a.ld = ld; a.cap = cap; a.below = nextafterf(cap, 0.0f);
     a.packed = (uint8_t *)d_ckpt;
     a.per_row = (Bp + 3) / 4;
     a.per_row_inv = 1.0 / (restore ? a.per_row : B);

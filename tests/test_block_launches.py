@@ -70,3 +70,16 @@ def test_a_lane_finds_its_columns_by_32_bits():
                         columns = (64 // int(m[1]) - 1) * b + b - 4
                         assert columns < 1 << 31 and 4 * columns < 1 << 32, (what, n, b, line)
     """)
+
+
+def test_which_blocks_are_read_past_the_caches():
+    """The backward pass over 48 2^20 values and more with tiles of 256 columns; narrower tiles (also where a quarter of the lanes of wide ones would be idle) never."""
+    routes.run(PTR + WIDE + """
+        for n, b, past in [(16384, 4096, True), (2101, 24001, True), (960, 52430, True), (3 << 14, 1 << 10, True), ((3 << 14) - 1, 1 << 10, False), (8192, 2048, False),
+                           (786433, 64, False), (50331648, 1, False), (393217, 128, False), (60000, 1030, True), (200000, 300, False)]:
+            (_, (rc, log)), (_, (rc8, log8)) = list(launches(n, b))[1:]
+            assert rc == rc8 == 0
+            for line in log + log8:
+                if "k_norm_grad" in line:
+                    assert line.split(", ")[2].startswith("true") == past, (n, b, line)
+    """)
