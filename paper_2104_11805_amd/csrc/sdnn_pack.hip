@@ -36,8 +36,9 @@ template <bool SIGNED> __device__ __forceinline__ void pack_group(const float (&
 }
 
 // What bounds it: 4 bytes read and one written a value.  A wavefront's half has two groups of the workgroup's stretch of 8 KB requested at a time, and reads past
-// the caches, so that they are left to the codes.  With k_unpack8 after it, 65536 x 1024 110 us (6.1 TB/s), 65536 x 4096 436; through the caches 111 and 489, one
-// group at a time strided by the grid 115 and 560.  Codes stored past the caches as well: k_pack8 59 -> 56 us, but k_unpack8 47 -> 67.
+// the caches, so that they are left to the codes.  65536 x 1024 66 us by itself (5.1 TB/s), 65536 x 4096 252.  With k_unpack8 after it, which reads part of the codes from
+// the caches, 104 to 110 us (6.1 to 6.5 TB/s) and 436; through the caches 111 and 489, one group at a time strided by the grid 115 and 560.  Codes stored past the caches as
+// well: 3 us less here, but 20 more in k_unpack8.
 template <bool SIGNED>
 __global__ void __launch_bounds__(256) k_pack8(const float *__restrict__ x, int64_t count, int64_t groups, float cap, uint8_t *__restrict__ packed)
 {
@@ -87,8 +88,8 @@ __global__ void __launch_bounds__(256) k_unpack8(const uint8_t *__restrict__ pac
 }
 
 // X_0 .. X_L of a training net, rows of ld floats, to and from one packed block after the other.  grid = (parts, blocks): blockIdx.y + l0 is l.
-// What bounds it: 4 bytes a value on one side, one on the other, after the chain from the layer's record to the block.  4 layers of 65536 neurons, 64 samples 24.6 us
-// into it and 17.9 out of it (4.3 and 5.9 TB/s), 16384 neurons and 255 samples (rows that are not whole fours) 31 and 26; 8 layers of 4096, 128 samples 8.1 and 6.1.
+// What bounds it: 4 bytes a value on one side, one on the other, after the chain from the layer's record to the block.  4 layers of 65536 neurons, 64 samples 24.4 us
+// into it and 17.7 out of it (4.3 and 5.9 TB/s), 16384 neurons and 255 samples (rows that are not whole fours) 31 and 26; 8 layers of 4096, 128 samples 8.1 and 6.1.
 struct NetBlocks {
     const LayerDev *layers;
     float *x0;
@@ -284,7 +285,7 @@ extern "C" int sdnn_pack8(const float *d_X, int32_t n, int32_t B, float cap, voi
     if (rc || n == 0) return rc;
     if (!d_X) return sdnn_fail(SDNN_EINVAL, "d_X is NULL");
     const int64_t count = (int64_t)n * B;
-    const dim3 grid((unsigned)std::min<int64_t>((pack8_groups(count) + 15) / 16, 16384)); // (8192: 2 us more of 59, no bound: 5 more)
+    const dim3 grid((unsigned)std::min<int64_t>((pack8_groups(count) + 15) / 16, 16384)); // (65536 x 1024: 8192 2 us more, no bound 5 more)
     if (cap > 0.0f) hipLaunchKernelGGL(k_pack8<false>, grid, dim3(256), 0, (hipStream_t)stream, d_X, count, pack8_groups(count), cap, (uint8_t *)d_packed);
     else hipLaunchKernelGGL(k_pack8<true>, grid, dim3(256), 0, (hipStream_t)stream, d_X, count, pack8_groups(count), cap, (uint8_t *)d_packed);
     return sdnn_launched();
