@@ -2846,11 +2846,11 @@ __global__ void __launch_bounds__(TR_THREADS) k_spread_vals(const LayerDev *__re
 }
 
 // The gradient that k_apply applies, for inspection, in CSR order: out[t_perm[q]] = g0[q] (+ g1[q]), the same
-// rounding as in k_apply.
+// rounding as in k_apply.  (Counters by the whole grid go up to 2^20 past the last of 2^31 - 1 entries: unsigned.)
 __global__ void __launch_bounds__(256) k_sum_parts(const float *__restrict__ g0, const float *__restrict__ g1,
                                                    const int32_t *__restrict__ perm, float *__restrict__ out, int n)
 {
-    for (int q = blockIdx.x * 256 + threadIdx.x; q < n; q += gridDim.x * 256) {
+    for (unsigned q = blockIdx.x * 256 + threadIdx.x; q < (unsigned)n; q += gridDim.x * 256) {
         double g = (double)g0[q];
         if (g1) g += (double)g1[q];
         out[perm[q]] = (float)g;
@@ -2863,7 +2863,7 @@ __global__ void __launch_bounds__(256) k_refresh_vals_t(const LayerDev *__restri
 {
     const LayerDev &L = layers[blockIdx.y];
     if (!L.vals_t) return;
-    for (int q = blockIdx.x * 256 + threadIdx.x; q < L.nnz; q += gridDim.x * 256) L.vals_t[q] = L.vals[L.t_perm[q]];
+    for (unsigned q = blockIdx.x * 256 + threadIdx.x; q < (unsigned)L.nnz; q += gridDim.x * 256) L.vals_t[q] = L.vals[L.t_perm[q]];
 }
 
 // The sum of a row of Delta over the samples, by 16 lanes (l: which of them), in all of them.
@@ -2919,7 +2919,7 @@ __global__ void __launch_bounds__(BLOCK_THREADS) k_hand_out(const LayerDev *__re
         }
         return;
     }
-    for (int q = (int)(blockIdx.x - bias_blocks) * BLOCK_THREADS + threadIdx.x; q < n; q += (int)(gridDim.x - bias_blocks) * BLOCK_THREADS) {
+    for (unsigned q = (blockIdx.x - bias_blocks) * BLOCK_THREADS + threadIdx.x; q < (unsigned)n; q += (gridDim.x - bias_blocks) * BLOCK_THREADS) {
         double g = (double)g0[q];
         if (g1) g += (double)g1[q];
         out[perm[q]] = (float)g;
@@ -5339,7 +5339,7 @@ static int backward_impl(sdnn_net *net, const float *d_dLoss, float *d_dX0, void
         for (const LayerDev &d : net->layers) max_nnz = std::max(max_nnz, d.nnz);
         for (int l0 = 0; l0 < L && max_nnz > 0; l0 += 65535) {
             const int nl = std::min(65535, L - l0);
-            hipLaunchKernelGGL(k_refresh_vals_t, dim3((unsigned)std::min(4096, (max_nnz + 2047) / 2048), (unsigned)nl), dim3(256), 0,
+            hipLaunchKernelGGL(k_refresh_vals_t, dim3((unsigned)std::min(4096, (max_nnz - 1) / 2048 + 1), (unsigned)nl), dim3(256), 0,
                                stream, net->d_layers + l0);
             HIP_TRY(net, hipGetLastError());
         }
@@ -5482,14 +5482,16 @@ static int launch_update(sdnn_net *net, int layer0, int n_layers, float lr, int 
     // One row / four, us: a layer of 352 rows of 32 entries 3.6 / 7.7, 1024 of 32 and 8 layers of them 3.5 / 6.5 and 21.6 / 24.6, 120 layers 138 / 128.
     // Parts 1 / 4 / 8: 609 rows of 50 entries in the mean, 133 samples 9.4 / 5.5 / 4.8; 4 layers of 1000 rows of 5 to 400 27.0 / 12.9 / -.
     int64_t nnz = 0, rows = 0;
-    int32_t longest = 0;
+    int32_t longest = 0, largest = 0;
     for (int l = layer0; l < layer0 + n_layers; ++l) {
         nnz += net->layers[l].nnz;
         rows += net->layers[l].n_out;
         longest = std::max(longest, net->max_len[0][l]);
+        largest = std::max(largest, net->layers[l].nnz);
     }
     const bool short_rows = nnz < 128 * rows;
-    const int rpw = short_rows && rows > 16384 ? 4 : 1, parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(8, (longest + 31) / 32), 16384 / rows));
+    const int rpw = short_rows && rows > 16384 ? 4 : 1, most_parts = largest > INT32_MAX - 512 ? 1 : 8; // (steps of 32 bits past a row's end)
+    const int parts = (int)std::max<int64_t>(1, std::min<int64_t>(std::min(most_parts, (longest - 1) / 32 + 1), 16384 / rows));
     const unsigned n_rg = (unsigned)((max_rows + UPD_WAVES * rpw - 1) / (UPD_WAVES * rpw));
     // with many layers, interleave them over the XCDs (one L2 per layer); with few, keep all XCDs on each layer
     const int interleave = n_layers >= 64;
@@ -5598,10 +5600,10 @@ extern "C" int sdnn_weight_grad(sdnn_net *net, int32_t layer, float *d_g, float 
         const int n = d_g && !spread ? d.nnz : 0;
         if (d_gb && d.n_out > 0) {
             const int bias_blocks = std::min(1 << 20, (d.n_out - 1) / (4 * WAVES_PER_BLOCK) + 1);
-            hipLaunchKernelGGL(k_hand_out, dim3((unsigned)(bias_blocks + std::min(4096, (n + BLOCK_THREADS - 1) / BLOCK_THREADS))), dim3(BLOCK_THREADS), 0, stream,
+            hipLaunchKernelGGL(k_hand_out, dim3((unsigned)(bias_blocks + std::min(4096, (int)(((int64_t)n + BLOCK_THREADS - 1) / BLOCK_THREADS)))), dim3(BLOCK_THREADS), 0, stream,
                                net->d_layers + (layer - 1), net->Bp, net->ld, d_gb, bias_blocks, g0, g1, d.t_perm, d_g, n);
         } else if (n > 0) {
-            hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)std::min(4096, (n + 255) / 256)), dim3(256), 0, stream, g0, g1, d.t_perm, d_g, n);
+            hipLaunchKernelGGL(k_sum_parts, dim3((unsigned)std::min(4096, (n - 1) / 256 + 1)), dim3(256), 0, stream, g0, g1, d.t_perm, d_g, n);
         }
         HIP_TRY(net, hipGetLastError());
         return SDNN_OK;
@@ -5668,7 +5670,7 @@ extern "C" int sdnn_set_weights(sdnn_net *net, int32_t layer, const float *d_val
     if (d_values) {
         rc = copy_dd(net, d.vals, d_values, 4 * (size_t)d.nnz, stream_);
         if (!rc && d.vals_t && d.nnz > 0) { // the transposed-order copy follows at once
-            hipLaunchKernelGGL(k_refresh_vals_t, dim3((unsigned)std::min(4096, (d.nnz + 2047) / 2048), 1u), dim3(256), 0,
+            hipLaunchKernelGGL(k_refresh_vals_t, dim3((unsigned)std::min(4096, (d.nnz - 1) / 2048 + 1), 1u), dim3(256), 0,
                                (hipStream_t)stream_, net->d_layers + (layer - 1));
             HIP_TRY(net, hipGetLastError());
         }
